@@ -47,7 +47,8 @@ typedef enum {
   NEZHA_ERR_CUDA = 4,            /* a CUDA runtime call failed; message in nezha_last_error                 */
   NEZHA_ERR_HASH_FULL = 5,       /* an insertion exhausted its probe bound                                  */
   NEZHA_ERR_CATALOG = 6,         /* a catalogue or history code outside [0, T_l)                            */
-  NEZHA_ERR_UNSUPPORTED = 7
+  NEZHA_ERR_UNSUPPORTED = 7,
+  NEZHA_ERR_PAGE = 8             /* paged cache: a page outside the pool, a length, row range or position out of bounds */
 } nezha_status;
 
 typedef struct {
@@ -267,6 +268,113 @@ nezha_status nezha_select(nezha_ctx* ctx, int32_t batch, int32_t n_beams, int32_
  * (Eq. 2-3).  Asynchronous. */
 nezha_status nezha_gemm(nezha_ctx* ctx, const void* A, const void* W, void* C, int32_t M, int32_t N, int32_t K,
                         int32_t epilogue, const float* bias, int32_t path);
+
+/* ---- operators over a paged context cache ------------------------------------------------------------------
+ * For servers that keep the keys and values of a user's history between requests, in a pool of fixed-size pages that all
+ * requests share: what a request adds is a chunk of new rows (the codes of the items since the last visit, the level's
+ * beams, one token) that is rotated, appended and attends to the whole history.  Element type: the context's storage type.
+ * One call is one layer.  The paper has no counterpart: it states the attention of its backbones by name only. */
+
+/* A pool of pages and, for a batch of sequences, which pages are theirs and which rows of the call are new.
+ * Position t of sequence b, KV head h:  k + page_table[b * table_stride + t / page_size] * page_stride + h * head_stride
+ * + (t % page_size) * pos_stride, head_dim consecutive elements (v alike).  Both nestings of head and position are strides.
+ * Sequence b's new rows are rows row_start[b] .. row_start[b + 1] - 1 of the call's matrices (none is legal) and its LAST
+ * positions: the last of them is position kv_len[b] - 1.  Rows outside [row_start[0], row_start[batch]) are left alone.
+ * Table entries behind the kv_len[b] positions are not read.
+ * Pool pointers and strides must be multiples of 16 bytes; no two (page, head, position) may overlap.
+ * Device contents are checked where they are used: a page outside [0, n_pages), a row range outside [0, rows] or not
+ * ascending, kv_len outside [0, max_kv] or more than max_new rows read as zeros or leave the sequence's rows alone, and the next
+ * synchronising call returns NEZHA_ERR_PAGE. */
+typedef struct {
+  void *k, *v;                   /* device                                                                   */
+  int64_t page_stride, head_stride, pos_stride;      /* elements                                              */
+  int32_t n_pages, page_size, n_kv_heads, head_dim;  /* head_dim 16, 32, 64 or 128                             */
+  const int32_t* page_table;     /* device [batch, table_stride], of which max_pages entries per sequence      */
+  int64_t table_stride;
+  int32_t max_pages, batch;
+  const int32_t* row_start;      /* device [batch + 1]                                                         */
+  const int32_t* kv_len;         /* device [batch] positions of each sequence, its new rows among them         */
+  int32_t rows;                  /* rows of the call's matrices                                                */
+  int32_t max_new, max_kv;       /* the most new rows and positions that a sequence may have; max_kv at most   */
+                                 /* max_pages * page_size.  They size the launch: tight bounds are faster       */
+} nezha_paged_kv;
+
+/* Rotary positions: angle of pair i (of rot_dim / 2) at position p = p * f_i, f_i = theta^(-2 i / rot_dim) before scaling. */
+#define NEZHA_ROPE_PLAIN 0
+#define NEZHA_ROPE_LINEAR 1      /* f_i / factor: positions interpolated                                        */
+#define NEZHA_ROPE_PARTS 2       /* interpolated by parts (Peng et al., 2023): pairs that turn at least turns_fast   */
+                                 /* times over trained_positions keep f_i, those that turn at most turns_slow times  */
+                                 /* get f_i / factor, a linear ramp over the pair index between them                 */
+typedef struct {
+  int32_t rot_dim;               /* leading dimensions of a head that are rotated, even, <= head_dim; the rest is copied */
+  int32_t interleaved;           /* pairs (i, i + rot_dim / 2): 0     pairs (2 i, 2 i + 1): 1                   */
+  float theta;
+  int32_t scaling;
+  float factor;                  /* >= 1 (LINEAR, PARTS)                                                       */
+  int32_t trained_positions;     /* PARTS                                                                      */
+  float turns_fast, turns_slow;  /* PARTS; both 0: 32 and 1                                                     */
+  float magnitude;               /* multiplies cosine and sine; 0: 1, for PARTS 0.1 ln(factor) + 1               */
+} nezha_rope;
+
+/* Cosines and sines of positions 0 .. n_positions - 1, angles in 64 bits:
+ *   table  device float [n_positions, rot_dim], 16-byte aligned: rot_dim / 2 cosines, then the sines.  Asynchronous. */
+nezha_status nezha_rope_table(nezha_ctx* ctx, const nezha_rope* rope, float* table, int32_t n_positions);
+
+/* Rotates the new rows of q and k by their positions and appends k and v to the pool, in one launch.
+ *   q, q_out  row i, head h at q + i * q_stride + h * head_dim (elements); q_out may be q itself.  Both NULL: no queries.
+ *   k, v      the same with n_kv_heads heads, e.g. columns of a fused QKV product
+ *   rope      NULL: nothing is rotated (q, if given, is copied).  Else table (nezha_rope_table, n_table positions)
+ *   positions device int32 [rows] or NULL: rotary position of each row where that is not its position in the sequence
+ * All pointers and strides must be multiples of 16 bytes.  Rounded once, to the storage type.  Two rows of one call
+ * must not share a place in the pool.  A row of which something is out of bounds is not written at all (NEZHA_ERR_PAGE).
+ * Asynchronous. */
+nezha_status nezha_kv_append(nezha_ctx* ctx, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads,
+                             void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             const nezha_rope* rope, const float* table, int32_t n_table, const int32_t* positions);
+
+/* What a row at position p sees of position t, and how:
+ *   score = scale * q.k;  softcap > 0: score = softcap * tanh(score / softcap);  slopes: score -= slopes[head] * |p - t|
+ *   causal 1: t <= p.  window > 0 (causal only): also t > p - window.  causal 0: every position of the sequence.
+ * (p = kv_len - new rows + index of the row; it may be negative: with causal 1 such a row sees nothing.) */
+typedef struct {
+  int32_t causal, window;
+  float scale, softcap;
+  const float* slopes;           /* device [n_q_heads] or NULL                                                 */
+} nezha_attn_form;
+
+/* Bytes of device workspace that nezha_paged_attention needs with these sizes (0: none; also on a bad argument).  Depends on
+ * the sizes in kv (batch, rows, max_new, max_kv, heads), n_q_heads and the device, on no device contents. */
+size_t nezha_paged_attention_workspace(nezha_ctx* ctx, const nezha_paged_kv* kv, int32_t n_q_heads, const nezha_attn_form* form);
+
+/* Softmax attention of the new rows over their sequences' positions in the pool (which nezha_kv_append has put there).
+ *   q, out     as in nezha_kv_append, n_q_heads a multiple of n_kv_heads (at most 64 per KV head); out must not overlap q or the pool
+ *   lse        device float [rows, n_q_heads] or NULL: natural log of the sum of the exponentials (-inf: nothing visible)
+ *   workspace  device, 256-byte aligned, nezha_paged_attention_workspace bytes (NULL if that is 0); in use until the call's
+ *              work is done.  Calls that can overlap need workspaces of their own.
+ * A row that sees nothing gets zeros.  Positions that a row does not see have no part in its result, whatever they hold.
+ * bf16: products of bf16 operands, sums, softmax statistics and the output's accumulator in 32 bits; the weights are rounded to bf16 for the
+ * second product, the result once.  The same call on the same contents returns the same bits.  Asynchronous. */
+nezha_status nezha_paged_attention(nezha_ctx* ctx, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads,
+                                   const nezha_attn_form* form, void* out, int64_t out_stride, float* lse,
+                                   void* workspace, size_t workspace_bytes);
+
+/* ---- 8-bit projections -------------------------------------------------------------------------------------
+ * A projection whose operands are 8-bit integers with a scale per row: per token for A, per output channel for W.  Half the
+ * bytes of bf16 weights, which is what a pass of few rows is bound by. */
+
+/* Rows to 8 bits: scale[m] = max|x[m, :]| / 127 (rounded once), q[m, k] = 127 x[m, k] / max|x[m, :]|, the exact quotient rounded
+ * to the nearest, halves to even.  A row of zeros: scale 0, q 0.  A row with an infinity or a NaN: scale NaN, q 0.
+ *   x  device, the context's storage type, row m at x + m * x_stride (elements)      q  device int8 [M, K]      scale  device float [M]
+ * For activations (M tokens) and, once, for weights (M output channels).  Asynchronous. */
+nezha_status nezha_quantize_rows(nezha_ctx* ctx, const void* x, int64_t x_stride, int32_t M, int32_t K, int8_t* q, float* scale);
+
+/* C[M, N] (op)= (sum_k A[m, k] W[n, k]) * a_scale[m] * w_scale[n] + bias[n]:  A int8 [M, K], W int8 [N, K], row-major and dense, -128 allowed.
+ * The sum is exact (32-bit integer; K at most 131071), the rest in fp32.
+ *   epilogue 0: C (storage type) = ;  1: C (float) = ;  2: C (float) +=           bias  device float [N] or NULL
+ * The counterpart of nezha_gemm, which documents M, N, K.  Every size is served; the tensor cores want A and W 16-byte aligned and
+ * K % 16 == 0.  The result does not depend on the kernel that serves it.  Asynchronous. */
+nezha_status nezha_gemm_int8(nezha_ctx* ctx, const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C,
+                             int32_t M, int32_t N, int32_t K, int32_t epilogue, const float* bias);
 
 /* ---- for callers that cannot allocate device memory (the paper has no counterpart) ------------------------ */
 

@@ -5,9 +5,12 @@ this module fails loudly when the library has not been built (there is no fallba
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import math
 import os
-from typing import Dict, Optional, Sequence
+from dataclasses import dataclass
+from typing import Dict, Optional, Sequence, Tuple
 
 import torch
 
@@ -21,7 +24,8 @@ MAX_LEVELS = 8
 MODE_DRAFT, MODE_VERIFIED, MODE_AR = 0, 1, 2
 OPT_DRAFT_TRANSITION, OPT_DRAFT_INPUTS, OPT_DRAFT_FILTER, OPT_FINAL_MASK, OPT_LEVEL_FILTER, OPT_ADAPTIVE_DRAFT = 0, 1, 2, 3, 4, 5
 STATUS_NAMES = ["OK", "ERR_ARG", "ERR_STATE", "ERR_ARENA_TOO_SMALL", "ERR_CUDA", "ERR_HASH_FULL", "ERR_CATALOG",
-                "ERR_UNSUPPORTED"]
+                "ERR_UNSUPPORTED", "ERR_PAGE"]
+ROPE_SCALINGS = {"none": 0, "linear": 1, "parts": 2}
 
 
 class NezhaConfig(C.Structure):
@@ -52,7 +56,23 @@ class NezhaTrace(C.Structure):
                 ("tree_codes", C.c_void_p), ("tree_count", C.c_void_p)]
 
 
-_vp, _i32, _sz = C.c_void_p, C.c_int32, C.c_size_t
+class NezhaPagedKV(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("pos_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("max_pages", C.c_int32), ("batch", C.c_int32),
+                ("row_start", C.c_void_p), ("kv_len", C.c_void_p), ("rows", C.c_int32), ("max_new", C.c_int32), ("max_kv", C.c_int32)]
+
+
+class NezhaRope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("theta", C.c_float), ("scaling", C.c_int32), ("factor", C.c_float),
+                ("trained_positions", C.c_int32), ("turns_fast", C.c_float), ("turns_slow", C.c_float), ("magnitude", C.c_float)]
+
+
+class NezhaAttnForm(C.Structure):
+    _fields_ = [("causal", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("softcap", C.c_float), ("slopes", C.c_void_p)]
+
+
+_vp, _i32, _i64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 lib.nezha_arena_bytes.restype = _sz
 lib.nezha_arena_bytes.argtypes = [C.POINTER(NezhaConfig), _sz, C.c_double]
 lib.nezha_create.restype = C.c_int
@@ -94,6 +114,18 @@ PROFILE_CLASSES = ["gemm", "attention", "select", "norm", "rope_append", "embed"
                    "accept", "hash", "misc"]
 lib.nezha_gemm.restype = C.c_int
 lib.nezha_gemm.argtypes = [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32]
+lib.nezha_rope_table.restype = C.c_int
+lib.nezha_rope_table.argtypes = [_vp, C.POINTER(NezhaRope), _vp, _i32]
+lib.nezha_kv_append.restype = C.c_int
+lib.nezha_kv_append.argtypes = [_vp, C.POINTER(NezhaPagedKV), _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, C.POINTER(NezhaRope), _vp, _i32, _vp]
+lib.nezha_paged_attention_workspace.restype = _sz
+lib.nezha_paged_attention_workspace.argtypes = [_vp, C.POINTER(NezhaPagedKV), _i32, C.POINTER(NezhaAttnForm)]
+lib.nezha_paged_attention.restype = C.c_int
+lib.nezha_paged_attention.argtypes = [_vp, C.POINTER(NezhaPagedKV), _vp, _i64, _i32, C.POINTER(NezhaAttnForm), _vp, _i64, _vp, _vp, _sz]
+lib.nezha_quantize_rows.restype = C.c_int
+lib.nezha_quantize_rows.argtypes = [_vp, _vp, _i64, _i32, _i32, _vp, _vp]
+lib.nezha_gemm_int8.restype = C.c_int
+lib.nezha_gemm_int8.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp]
 lib.nezha_launch_count.restype = C.c_uint64
 lib.nezha_launch_count.argtypes = []
 lib.nezha_profile_enable.restype = C.c_int
@@ -111,7 +143,8 @@ NOALLOC_MAX_TUPLES = 1 << 20
 EXPORTS = ["nezha_arena_bytes", "nezha_create", "nezha_build_hashset", "nezha_pack", "nezha_probe",
            "nezha_contains_noalloc", "nezha_prefill",
            "nezha_decode", "nezha_decode_with_drafts", "nezha_decode_with_draft_tree", "nezha_set_option", "nezha_get_hidden", "nezha_primary_logits",
-           "nezha_draft_logits", "nezha_select", "nezha_gemm", "nezha_launch_count", "nezha_profile_enable",
+           "nezha_draft_logits", "nezha_select", "nezha_gemm", "nezha_rope_table", "nezha_kv_append",
+           "nezha_paged_attention_workspace", "nezha_paged_attention", "nezha_quantize_rows", "nezha_gemm_int8", "nezha_launch_count", "nezha_profile_enable",
            "nezha_profile_read", "nezha_sync", "nezha_last_error", "nezha_destroy"]
 
 
@@ -148,6 +181,64 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _ptr_array(ts: Sequence[torch.Tensor]):
     arr = (C.c_void_p * len(ts))(*[_ptr(t) for t in ts])
     return C.cast(arr, _PP), arr
+
+
+@dataclass
+class Rope:
+    """nezha_rope: rotary positions of the first `rot_dim` dimensions of a head, scaled for long contexts or not."""
+    rot_dim: int
+    theta: float = 10000.0
+    interleaved: bool = False
+    scaling: str = "none"                 # a key of ROPE_SCALINGS
+    factor: float = 1.0
+    trained_positions: int = 0
+    turns_fast: float = 0.0
+    turns_slow: float = 0.0
+    magnitude: float = 0.0
+
+    def struct(self) -> NezhaRope:
+        return NezhaRope(self.rot_dim, int(self.interleaved), self.theta, ROPE_SCALINGS[self.scaling], self.factor, self.trained_positions,
+                         self.turns_fast, self.turns_slow, self.magnitude)
+
+
+@dataclass
+class RopeTable:
+    """What Engine.rope_table returns: the cosines and sines of positions 0 .. n - 1, float32 [n, rot_dim]."""
+    rope: Rope
+    table: torch.Tensor
+
+
+class PagedKV:
+    """nezha_paged_kv: a pool of pages, and a batch's page table, lengths and new rows (all device tensors; kept alive here).
+
+    k_pool, v_pool  [n_pages, n_kv_heads, page_size, head_dim], any strides with a dense last dimension: a pool that keeps positions
+                    outside heads is passed as `pool.transpose(1, 2)`; the two have the same strides
+    page_table      int32 [batch, max_pages]
+    row_start       int32 [batch + 1], kv_len int32 [batch]
+    max_new, max_kv the most new rows and positions of a sequence (default: all rows of the call, all positions of the table)
+    """
+
+    def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor,
+                 max_new: Optional[int] = None, max_kv: Optional[int] = None):
+        assert k_pool.dim() == 4 and k_pool.shape == v_pool.shape and k_pool.dtype == v_pool.dtype
+        assert k_pool.stride() == v_pool.stride() and k_pool.stride(3) == 1
+        assert page_table.dim() == 2 and page_table.stride(1) == 1 and row_start.is_contiguous() and kv_len.is_contiguous()
+        assert page_table.dtype == row_start.dtype == kv_len.dtype == torch.int32
+        batch, max_pages = page_table.shape
+        assert tuple(row_start.shape) == (batch + 1,) and tuple(kv_len.shape) == (batch,)
+        for t in (v_pool, page_table, row_start, kv_len):
+            assert t.device == k_pool.device and t.is_cuda
+        self.k_pool, self.v_pool, self.page_table, self.row_start, self.kv_len = k_pool, v_pool, page_table, row_start, kv_len
+        n_pages, heads, page_size, hd = k_pool.shape
+        self.max_new, self.max_kv = max_new, max_pages * page_size if max_kv is None else max_kv
+        st = k_pool.stride()
+        self._s = NezhaPagedKV(k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
+                               max(page_table.stride(0), max_pages), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr(), 0, 0, self.max_kv)
+
+    def struct(self, rows: int) -> NezhaPagedKV:
+        self._s.rows = rows
+        self._s.max_new = rows if self.max_new is None else min(self.max_new, rows)
+        return self._s
 
 
 class Engine:
@@ -344,6 +435,107 @@ class Engine:
         N = W.shape[0]
         assert W.shape[1] == K and tuple(C_out.shape) == (M, N)
         self._check(lib.nezha_gemm(self._h, _ptr(A), _ptr(W), _ptr(C_out), M, N, K, epilogue, _ptr(bias), path))
+        return C_out
+
+    # -- operators over a paged context cache, 8-bit projections --------------------------------------------
+    @property
+    def dtype(self) -> torch.dtype:
+        return torch.bfloat16 if self.cfg.dtype == 1 else torch.float32
+
+    def _on_stream(self):
+        """Buffers that a method makes belong to the engine's stream, whatever stream is current."""
+        mine = torch.cuda.default_stream(self.arena.device) if self.stream is None else self.stream
+        return contextlib.nullcontext() if torch.cuda.current_stream(self.arena.device) == mine else torch.cuda.stream(mine)
+
+    def _rows(self, t: torch.Tensor, heads: Optional[int], hd: int, rows: Optional[int]) -> Tuple[int, int]:
+        """(pointer, row stride) of [rows, heads, hd] whose heads lie side by side."""
+        assert t.dim() == 3 and t.shape[2] == hd and (heads is None or t.shape[1] == heads) and (rows is None or t.shape[0] == rows)
+        assert t.dtype == self.dtype and t.device == self.arena.device
+        assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == hd)
+        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * hd)
+
+    def rope_table(self, rope: Rope, n_positions: int) -> RopeTable:
+        with self._on_stream():
+            table = torch.empty(n_positions, rope.rot_dim, dtype=torch.float32, device=self.arena.device)
+        self._check(lib.nezha_rope_table(self._h, C.byref(rope.struct()), table.data_ptr(), n_positions))
+        return RopeTable(rope, table)
+
+    def kv_append(self, kv: PagedKV, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None,
+                  positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """k, v [rows, n_kv_heads, head_dim] (and q [rows, n_q_heads, head_dim]) of the new rows, e.g. slices of a fused QKV product.
+        Returns the rotated q (q_out, a new tensor if not given; q itself is legal)."""
+        _, heads, _, hd = kv.k_pool.shape
+        rows = int(k.shape[0])
+        assert kv.k_pool.dtype == self.dtype
+        kp, ks = self._rows(k, heads, hd, None)
+        vp, vs = self._rows(v, heads, hd, rows)
+        qp = qs = op = os_ = None
+        if q is not None:
+            qp, qs = self._rows(q, None, hd, rows)
+            if q_out is None:
+                with self._on_stream():
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            op, os_ = self._rows(q_out, q.shape[1], hd, rows)
+        assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == rows)
+        table = None if rope is None else rope.table
+        st = lib.nezha_kv_append(self._h, C.byref(kv.struct(rows)), qp, qs or 0, 0 if q is None else q.shape[1], op, os_ or 0, kp, ks, vp, vs,
+                                 None if rope is None else C.byref(rope.rope.struct()), _ptr(table), 0 if table is None else table.shape[0],
+                                 _ptr(positions))
+        if st:
+            self._check(st)
+        return q_out
+
+    def paged_attention(self, kv: PagedKV, q: torch.Tensor, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                        softcap: float = 0.0, slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the new rows q [rows, n_q_heads, head_dim] over their sequences' positions; scale: 1 / sqrt(head_dim) if not given;
+        lse: float32 [rows, n_q_heads] to fill.  The workspace, where one is needed, is a new tensor of the call."""
+        rows, heads, hd = q.shape
+        assert hd == kv.k_pool.shape[3] and kv.k_pool.dtype == self.dtype
+        qp, qs = self._rows(q, None, hd, None)
+        assert slopes is None or (slopes.dtype == torch.float32 and slopes.numel() == heads)
+        assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (rows, heads))
+        form = NezhaAttnForm(int(causal), window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, _ptr(slopes))
+        s = kv.struct(rows)
+        need = lib.nezha_paged_attention_workspace(self._h, C.byref(s), heads, C.byref(form))
+        ws = None
+        if out is None or need:
+            with self._on_stream():
+                if out is None:
+                    out = torch.empty(rows, heads, hd, dtype=q.dtype, device=q.device)
+                if need:
+                    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        op, os_ = self._rows(out, heads, hd, rows)
+        st = lib.nezha_paged_attention(self._h, C.byref(s), qp, qs, heads, C.byref(form), op, os_, _ptr(lse), _ptr(ws), need)
+        if st:
+            self._check(st)
+        return out
+
+    def quantize_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """x [M, K] -> (int8 [M, K], float32 [M]); rows of x may be strided."""
+        M, K = x.shape
+        assert x.dtype == self.dtype and x.device == self.arena.device and (x.stride(1) == 1 or K == 1)
+        if q is None or scale is None:
+            with self._on_stream():
+                q = torch.empty(M, K, dtype=torch.int8, device=x.device) if q is None else q
+                scale = torch.empty(M, dtype=torch.float32, device=x.device) if scale is None else scale
+        assert q.dtype == torch.int8 and tuple(q.shape) == (M, K) and scale.dtype == torch.float32 and scale.numel() == M
+        st = lib.nezha_quantize_rows(self._h, x.data_ptr(), x.stride(0) if M > 1 else max(x.stride(0), K), M, K, _ptr(q), _ptr(scale))
+        if st:
+            self._check(st)
+        return q, scale
+
+    def gemm_int8(self, A: torch.Tensor, a_scale: torch.Tensor, W: torch.Tensor, w_scale: torch.Tensor, C_out: torch.Tensor, epilogue: int = 0,
+                  bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+        M, K = A.shape
+        N = W.shape[0]
+        assert A.dtype == W.dtype == torch.int8 and W.shape[1] == K and tuple(C_out.shape) == (M, N)
+        assert C_out.dtype == (self.dtype if epilogue == 0 else torch.float32)
+        assert a_scale.dtype == w_scale.dtype == torch.float32 and a_scale.numel() == M and w_scale.numel() == N
+        assert bias is None or (bias.dtype == torch.float32 and bias.numel() == N)
+        st = lib.nezha_gemm_int8(self._h, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(C_out), M, N, K, epilogue, _ptr(bias))
+        if st:
+            self._check(st)
         return C_out
 
     def profile_enable(self, on: bool):

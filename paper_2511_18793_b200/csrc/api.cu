@@ -6,12 +6,14 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <map>
 #include <string>
 #include <vector>
 
 #include "common.cuh"
 #include "engine_state.cuh"
+#include "operators.cuh"
 
 namespace nz {
 void launch_hs_pack(const LevelInfo& li, const int* codes, unsigned long long n, unsigned long long* keys, int* status,
@@ -625,6 +627,7 @@ nezha_status device_error(nezha_ctx* c, const int* words) {
   if (st) NZ_CUDA(c, cudaMemsetAsync(c->es.status, 0, 4 * sizeof(int), c->st));
   if (st & kStHashFull) return fail(c, NEZHA_ERR_HASH_FULL, "hash set insertion exhausted its probe bound");
   if (st & kStBadCode) return fail(c, NEZHA_ERR_CATALOG, "a code outside [0, T_l) was given");
+  if (st & kStBadPage) return fail(c, NEZHA_ERR_PAGE, "paged cache: a page outside the pool, or a length, row range or position out of bounds");
   if (st)      // a kernel that records where it gave up leaves three more words (0 if it does not)
     return fail(c, NEZHA_ERR_CUDA, "a bounded device-side wait expired (kernel gave up and returned); where: " +
                                        std::to_string(words[1]) + " " + std::to_string(words[2]) + " " + std::to_string(words[3]));
@@ -1162,6 +1165,204 @@ nezha_status nezha_gemm(nezha_ctx* c, const void* A, const void* W, void* C, int
   if (path >= 2 && !tc_ok) return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm: shape not covered by the tcgen05 kernel");
   if (path != 1 && tc_ok) launch_gemm_tc(a, c->st);
   else launch_gemm_simt(a, c->bf16, c->st);
+  NZ_CUDA(c, cudaGetLastError());
+  return NEZHA_OK;
+}
+
+// ---- operators over a paged context cache, and 8-bit projections ----------------------------------------
+namespace {
+
+// The context's GPU has to be the current device (a launch goes to the current one).
+nezha_status check_device(nezha_ctx* c, const char* who) {
+  int dev = -1;
+  NZ_CUDA(c, cudaGetDevice(&dev));
+  if (dev != c->device) return fail(c, NEZHA_ERR_ARG, std::string(who) + ": the context's GPU must be the current device");
+  return NEZHA_OK;
+}
+
+// Null if rows of `width` elements, `stride` apart, can be read and written in 16-byte pieces.
+const char* rows_fault(const nezha_ctx* c, const void* p, int64_t stride, int64_t width, const char* what) {
+  static thread_local std::string msg;
+  if (!p) return (msg = std::string("null ") + what).c_str();
+  if (((uintptr_t)p & 15) || (stride * (int64_t)c->esz) % 16) return (msg = std::string(what) + " not aligned to 16 bytes").c_str();
+  if (stride < width) return (msg = std::string(what) + ": rows overlap").c_str();
+  return nullptr;
+}
+
+// What is wrong with a paged cache's description, or null.
+const char* paged_fault(const nezha_ctx* c, const nezha_paged_kv* p) {
+  if (!p) return "null cache";
+  if (!p->k || !p->v || !p->page_table || !p->row_start || !p->kv_len) return "null pointer in the cache";
+  if (p->head_dim != 16 && p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 16, 32, 64 or 128";
+  if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1 || p->batch < 1 || p->max_pages < 1) return "a size of the cache is not positive";
+  if (p->table_stride < p->max_pages) return "table_stride below max_pages";
+  if (p->rows < 0 || p->max_new < 0 || p->max_new > p->rows) return "rows, max_new out of range";
+  if (p->max_kv < 0 || (int64_t)p->max_kv > (int64_t)p->max_pages * p->page_size) return "max_kv beyond max_pages * page_size";
+  if (((uintptr_t)p->k & 15) || ((uintptr_t)p->v & 15)) return "pool not aligned to 16 bytes";
+  // every extent of more than one step: strides in 16-byte pieces, and none shorter than what the smaller ones span
+  struct Dim { int64_t stride, n; } d[3] = {{p->page_stride, p->n_pages}, {p->head_stride, p->n_kv_heads}, {p->pos_stride, p->page_size}};
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  int64_t span = p->head_dim;
+  for (const Dim& x : d) {
+    if (x.n == 1) continue;
+    if (x.stride < span) return "positions of the pool overlap";
+    if ((x.stride * (int64_t)c->esz) % 16) return "pool strides not multiples of 16 bytes";
+    if (x.stride > (INT64_MAX / 16) / x.n) return "pool strides out of range";
+    span = x.stride * (x.n - 1) + span;
+  }
+  return nullptr;
+}
+
+PagedView paged_view(nezha_ctx* c, const nezha_paged_kv* p) {
+  return PagedView{p->k, p->v, p->page_stride, p->head_stride, p->pos_stride, p->n_pages, p->page_size, p->n_kv_heads, p->head_dim, p->page_table,
+                   p->table_stride, p->max_pages, p->batch, p->row_start, p->kv_len, p->rows, p->max_new, p->max_kv, c->es.status};
+}
+
+const char* rope_fault(const nezha_rope* r) {
+  if (!r) return "null rope";
+  if (r->rot_dim < 2 || r->rot_dim > 128 || r->rot_dim % 2) return "rot_dim must be even, 2 to 128";
+  if (r->interleaved != 0 && r->interleaved != 1) return "interleaved must be 0 or 1";
+  if (!(r->theta > 1.f) || !std::isfinite(r->theta)) return "theta must be above 1";
+  if (r->scaling < NEZHA_ROPE_PLAIN || r->scaling > NEZHA_ROPE_PARTS) return "unknown scaling";
+  if (r->scaling != NEZHA_ROPE_PLAIN && (!(r->factor >= 1.f) || !std::isfinite(r->factor))) return "factor must be at least 1";
+  if (!(r->magnitude >= 0.f) || !std::isfinite(r->magnitude)) return "magnitude must not be negative";
+  if (r->scaling == NEZHA_ROPE_PARTS) {
+    if (r->trained_positions < 1) return "trained_positions must be positive";
+    const bool given = r->turns_fast != 0.f || r->turns_slow != 0.f;
+    if (given && (!(r->turns_slow > 0.f) || !(r->turns_fast > r->turns_slow) || !std::isfinite(r->turns_fast))) return "turns_fast must be above turns_slow, and that above 0";
+  }
+  return nullptr;
+}
+
+const char* attn_fault(const nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq, const nezha_attn_form* f) {
+  if (const char* why = paged_fault(c, kv)) return why;
+  if (!f) return "null form";
+  if (Hq < 1 || Hq % kv->n_kv_heads || Hq / kv->n_kv_heads > 64) return "n_q_heads must be a multiple of n_kv_heads, at most 64 times it";
+  if (f->causal != 0 && f->causal != 1) return "causal must be 0 or 1";
+  if (f->window < 0 || (f->window > 0 && !f->causal)) return "a window must be positive, and causal";
+  if (!std::isfinite(f->scale)) return "scale must be finite";
+  if (!(f->softcap >= 0.f) || !std::isfinite(f->softcap)) return "softcap must not be negative";
+  // a launch has a CTA per (KV head, row tile, split, sequence)
+  if ((double)kv->n_kv_heads * kv->batch * ((double)kv->max_new * (Hq / kv->n_kv_heads) / 16 + 1) > 2e8 || (int64_t)kv->rows * Hq > INT32_MAX)
+    return "too many sequences, heads and rows for one call";
+  return nullptr;
+}
+
+PagedAttnArgs attn_args(nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq, const nezha_attn_form* f) {
+  PagedAttnArgs a{};
+  a.kv = paged_view(c, kv);
+  a.Hq = Hq; a.G = Hq / kv->n_kv_heads;
+  a.scale = f->scale; a.softcap = f->softcap; a.slopes = f->slopes; a.causal = f->causal; a.window = f->window;
+  a.splits = 1;
+  return a;
+}
+
+}  // namespace
+
+nezha_status nezha_rope_table(nezha_ctx* c, const nezha_rope* r, float* table, int32_t n_positions) {
+  if (!c) return NEZHA_ERR_ARG;
+  const char* why = rope_fault(r);
+  if (!why && (!table || ((uintptr_t)table & 15))) why = "table null or not aligned to 16 bytes";
+  if (!why && n_positions < 0) why = "n_positions negative";
+  if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_rope_table: ") + why);
+  if (const nezha_status s = check_device(c, "nezha_rope_table")) return s;
+  if (!n_positions) return NEZHA_OK;
+  RopeFrequencies f{};
+  f.half = r->rot_dim / 2;
+  const double factor = r->scaling == NEZHA_ROPE_PLAIN ? 1.0 : (double)r->factor;
+  f.magnitude = r->magnitude > 0.f ? (double)r->magnitude : r->scaling == NEZHA_ROPE_PARTS ? 0.1 * log(factor) + 1.0 : 1.0;
+  const double fast = r->turns_fast != 0.f ? r->turns_fast : 32.0, slow = r->turns_fast != 0.f ? r->turns_slow : 1.0;
+  const double two_pi = 6.283185307179586476925;
+  // the pair that turns n times over the trained positions
+  auto pair_of = [&](double n) { return r->rot_dim * log(r->trained_positions / (n * two_pi)) / (2.0 * log((double)r->theta)); };
+  const double lo = r->scaling == NEZHA_ROPE_PARTS ? std::max(floor(pair_of(fast)), 0.0) : 0.0;
+  const double hi = r->scaling == NEZHA_ROPE_PARTS ? std::min(ceil(pair_of(slow)), r->rot_dim - 1.0) : 0.0;
+  for (int i = 0; i < f.half; ++i) {
+    const double plain = pow((double)r->theta, -2.0 * i / r->rot_dim);
+    double share = r->scaling == NEZHA_ROPE_LINEAR ? 1.0 : 0.0;      // of the interpolated frequency
+    if (r->scaling == NEZHA_ROPE_PARTS) share = std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
+    f.f[i] = plain * (1.0 - share) + plain / factor * share;
+  }
+  launch_rope_table(f, table, n_positions, c->st);
+  NZ_CUDA(c, cudaGetLastError());
+  return NEZHA_OK;
+}
+
+nezha_status nezha_kv_append(nezha_ctx* c, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out,
+                             int64_t q_out_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, const nezha_rope* rope,
+                             const float* table, int32_t n_table, const int32_t* positions) {
+  if (!c) return NEZHA_ERR_ARG;
+  const char* why = paged_fault(c, kv);
+  const int64_t kv_width = why ? 0 : (int64_t)kv->n_kv_heads * kv->head_dim;
+  if (!why) why = rows_fault(c, k, k_stride, kv_width, "k");
+  if (!why) why = rows_fault(c, v, v_stride, kv_width, "v");
+  if (!why && (!q != !q_out)) why = "q and q_out must both be given, or neither";
+  if (!why && q && n_q_heads < 1) why = "n_q_heads must be positive";
+  if (!why && q) why = rows_fault(c, q, q_stride, (int64_t)n_q_heads * kv->head_dim, "q");
+  if (!why && q) why = rows_fault(c, q_out, q_out_stride, (int64_t)n_q_heads * kv->head_dim, "q_out");
+  if (!why && q == q_out && q && q_stride != q_out_stride) why = "q_out on q with another stride";
+  if (!why && rope) {
+    why = rope_fault(rope);
+    if (!why && rope->rot_dim > kv->head_dim) why = "rot_dim above head_dim";
+    if (!why && (!table || ((uintptr_t)table & 15) || n_table < 1)) why = "table null, empty or not aligned to 16 bytes";
+  }
+  if (!why && (int64_t)((q ? n_q_heads : 0) + 2 * kv->n_kv_heads) * kv->head_dim > (1 << 24)) why = "too many heads";
+  if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_kv_append: ") + why);
+  if (const nezha_status s = check_device(c, "nezha_kv_append")) return s;
+  if (!kv->rows) return NEZHA_OK;
+  AppendArgs a{paged_view(c, kv), q, q_stride, q ? n_q_heads : 0, q_out, q_out_stride, k, k_stride, v, v_stride,
+               rope ? rope->rot_dim : 0, rope ? rope->interleaved : 0, table, rope ? n_table : 0, positions};
+  launch_kv_append(a, c->bf16, c->st);
+  NZ_CUDA(c, cudaGetLastError());
+  return NEZHA_OK;
+}
+
+size_t nezha_paged_attention_workspace(nezha_ctx* c, const nezha_paged_kv* kv, int32_t n_q_heads, const nezha_attn_form* form) {
+  if (!c || attn_fault(c, kv, n_q_heads, form)) return 0;
+  return paged_attn_plan(attn_args(c, kv, n_q_heads, form), c->bf16).bytes;
+}
+
+nezha_status nezha_paged_attention(nezha_ctx* c, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads,
+                                   const nezha_attn_form* form, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes) {
+  if (!c) return NEZHA_ERR_ARG;
+  const char* why = attn_fault(c, kv, n_q_heads, form);
+  if (!why) why = rows_fault(c, q, q_stride, (int64_t)n_q_heads * kv->head_dim, "q");
+  if (!why) why = rows_fault(c, out, out_stride, (int64_t)n_q_heads * kv->head_dim, "out");
+  if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_paged_attention: ") + why);
+  if (const nezha_status s = check_device(c, "nezha_paged_attention")) return s;
+  if (!kv->max_new) return NEZHA_OK;
+  PagedAttnArgs a = attn_args(c, kv, n_q_heads, form);
+  a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
+  const PagedAttnPlan plan = paged_attn_plan(a, c->bf16);
+  if (plan.bytes && (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < plan.bytes))
+    return fail(c, NEZHA_ERR_ARG, "nezha_paged_attention: workspace null, not aligned to 256 bytes or smaller than nezha_paged_attention_workspace says");
+  a.part_o = (float*)workspace;
+  launch_paged_attention(a, plan, c->bf16, c->st);
+  NZ_CUDA(c, cudaGetLastError());
+  return NEZHA_OK;
+}
+
+nezha_status nezha_quantize_rows(nezha_ctx* c, const void* x, int64_t x_stride, int32_t M, int32_t K, int8_t* q, float* scale) {
+  if (!c) return NEZHA_ERR_ARG;
+  if (!x || !q || !scale || M < 0 || K < 1 || x_stride < K) return fail(c, NEZHA_ERR_ARG, "nezha_quantize_rows: bad argument");
+  if (const nezha_status s = check_device(c, "nezha_quantize_rows")) return s;
+  if (!M) return NEZHA_OK;
+  launch_quantize_rows(x, x_stride, M, K, q, scale, c->bf16, c->st);
+  NZ_CUDA(c, cudaGetLastError());
+  return NEZHA_OK;
+}
+
+nezha_status nezha_gemm_int8(nezha_ctx* c, const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C, int32_t M,
+                             int32_t N, int32_t K, int32_t epilogue, const float* bias) {
+  if (!c) return NEZHA_ERR_ARG;
+  if (!A || !a_scale || !W || !w_scale || !C || M < 1 || N < 1 || K < 1 || epilogue < 0 || epilogue > 2)
+    return fail(c, NEZHA_ERR_ARG, "nezha_gemm_int8: bad argument");
+  if (K > 131071) return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm_int8: sums of more than 131071 products do not fit 32 bits");
+  if ((int64_t)((M + 63) / 64) * ((N + 63) / 64) > INT32_MAX) return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm_int8: product too large for one call");
+  if (((uintptr_t)C % (epilogue == 0 ? c->esz : 4)) || ((uintptr_t)a_scale & 3) || ((uintptr_t)w_scale & 3) || ((uintptr_t)bias & 3))
+    return fail(c, NEZHA_ERR_ARG, "nezha_gemm_int8: a pointer is not aligned to its element");
+  if (const nezha_status s = check_device(c, "nezha_gemm_int8")) return s;
+  launch_gemm_i8(GemmI8Args{A, W, a_scale, w_scale, bias, C, M, N, K, epilogue, c->es.status}, c->bf16, c->st);
   NZ_CUDA(c, cudaGetLastError());
   return NEZHA_OK;
 }

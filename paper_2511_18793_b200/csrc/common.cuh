@@ -16,7 +16,7 @@ constexpr unsigned long long kEmptyKey = ~0ull;  // never a packed key: prod(T) 
 constexpr int kMaxProbeBuckets = 4096;           // bound of every probe / insert walk
 
 // bits of the device status word
-enum : int { kStHashFull = 1, kStBadCode = 2, kStInternal = 4 };
+enum : int { kStHashFull = 1, kStBadCode = 2, kStInternal = 4, kStBadPage = 8 };
 
 // Kernel classes for the launch counter and the optional CUDA-event timing (see nezha_profile_*).
 enum KernelClass : int {
