@@ -57,8 +57,7 @@ __global__ void __launch_bounds__(256) gemm_i8_simt_kernel(GemmI8Args a, int til
 
 }  // namespace
 
-void launch_gemm_i8(const GemmI8Args& a, bool bf16, cudaStream_t st) {
-  LaunchScope ls(kcGemm, st);
+void launch_gemm_i8_simt(const GemmI8Args& a, bool bf16, cudaStream_t st) {
   const int tiles_n = (a.N + kT - 1) / kT;
   const dim3 grid((unsigned)((long long)((a.M + kT - 1) / kT) * tiles_n));
   if (a.epilogue == kEpiAddF32) launch_pdl(gemm_i8_simt_kernel<float, true>, grid, dim3(256), 0, st, a, tiles_n);

@@ -7,15 +7,19 @@
 // row tile and not once per head.  A context is split over CTAs where sequences, heads and row tiles leave SMs idle; the parts
 // (their own maximum and sum: o and log2 of the sum) are joined by attn_join_kernel in the order of the splits.
 #include <math.h>
+#include <stdlib.h>
 
 #include "operators.cuh"
 
 namespace nz {
 
 int sm_count();
+void launch_paged_attn_tc(const PagedAttnArgs& a, int rows, cudaStream_t st);
 
 namespace {
 
+enum { kSimt = 0, kTc16 = 1, kTc64 = 2 };
+constexpr int kMaxSplits = 64;
 constexpr int kRowsS = 16, kPosS = 32, kWarpsS = 4, kRowsWarp = kRowsS / kWarpsS;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -148,15 +152,25 @@ __global__ void __launch_bounds__(32 * kWarpsS) paged_attn_simt_kernel(PagedAttn
   }
 }
 
-// A warp per (row, head): the parts in the order of the splits, weighted by their sums.
+// A block per (row, head): the parts weighted by their sums.  Warp w adds the parts w, w + 4, ... in their order, all of whose loads are under way
+// together (a warp per row and head that skipped empty parts by a branch: one load at a time, 57 parts 20 us), the four sums are added in order.
+constexpr int kJoinWarps = 4;
 template <typename T, int HD>
-__global__ void attn_join_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArgs a) {
+  __shared__ float sums[kJoinWarps][HD];
   pdl_wait();
   pdl_launch();
-  const long long rh = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  const long long rh = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = (int)(rh / a.Hq), head = (int)(rh - (long long)row * a.Hq);
-  if (row >= a.kv.rows) return;
+  // a lane looks after two parts' weights (kMaxSplits of them at most)
+  const long long n = (long long)a.kv.rows * a.Hq;
+  float w[2], m = -INFINITY;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = lane + 32 * h;
+    w[h] = i < a.splits ? a.part_lse[i * n + rh] : -INFINITY;
+  }
   // rows that no sequence has are left alone (a split wrote nothing for them)
   int lo = 0, hi = a.kv.batch + 1;
   while (lo < hi) {
@@ -169,31 +183,49 @@ __global__ void attn_join_kernel(PagedAttnArgs a) {
   if (lo < 1 || lo > a.kv.batch) return;
   const PagedSeq s = paged_seq(a.kv, lo - 1, false);
   if (row < s.row0 || row >= s.row0 + s.n) return;
-  const long long n = (long long)a.kv.rows * a.Hq;
-  float m = -INFINITY;
-  for (int i = 0; i < a.splits; ++i) {
-    const float x = a.part_lse[i * n + rh];
-    m = x > m || x != x ? x : m;                   // a NaN stays
+  m = warp_max(fmaxf(w[0], w[1]));
+  const bool none = m == -INFINITY && !__any_sync(0xffffffffu, w[0] != w[0] || w[1] != w[1]);
+  unsigned seen[2];
+  float sum = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    seen[h] = __ballot_sync(0xffffffffu, w[h] != -INFINITY);
+    w[h] = w[h] == -INFINITY ? 0.f : exp2f(w[h] - m);      // (a NaN stays one)
+    sum += w[h];
   }
+  sum = warp_sum(sum);
   constexpr int DL = HD >= 32 ? HD / 32 : 1;
-  float o[DL], sum = 0.f;
+  float o[DL];
 #pragma unroll
   for (int d = 0; d < DL; ++d) o[d] = 0.f;
-  for (int i = 0; i < a.splits; ++i) {
-    const float x = a.part_lse[i * n + rh];
-    if (x == -INFINITY) continue;
-    const float w = exp2f(x - m);
-    sum += w;
+  const int col = HD >= 32 ? lane * DL : lane & 15;
 #pragma unroll
-    for (int d = 0; d < DL; ++d)
-      if (HD >= 32 || lane < 16) o[d] = fmaf(w, a.part_o[(i * n + rh) * HD + lane + 32 * d], o[d]);
+  for (int j = 0; j < kMaxSplits / kJoinWarps; ++j) {
+    const int i = warp + kJoinWarps * j;
+    if (i >= a.splits) break;
+    const float wi = __shfl_sync(0xffffffffu, i < 32 ? w[0] : w[1], i & 31);
+    const bool on = (i < 32 ? seen[0] : seen[1]) >> (i & 31) & 1u;          // (else nothing was written for it)
+    const float* part = a.part_o + (i * n + rh) * HD + col;
+    float x[DL];
+    if constexpr (DL == 4) { const float4 v = on ? *reinterpret_cast<const float4*>(part) : make_float4(0.f, 0.f, 0.f, 0.f); x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+    else if constexpr (DL == 2) { const float2 v = on ? *reinterpret_cast<const float2*>(part) : make_float2(0.f, 0.f); x[0] = v.x; x[1] = v.y; }
+    else x[0] = on ? *part : 0.f;
+#pragma unroll
+    for (int d = 0; d < DL; ++d) o[d] = fmaf(wi, x[d], o[d]);
   }
-  const float inv = m == -INFINITY ? 0.f : 1.f / sum;
-  T* out = (T*)a.out + row * a.out_stride + (long long)head * HD;
+  if (HD >= 32 || lane < 16)
 #pragma unroll
-  for (int d = 0; d < DL; ++d)
-    if (HD >= 32 || lane < 16) out[lane + 32 * d] = from_f32<T>(o[d] * inv);
-  if (a.lse && lane == 0) a.lse[rh] = m == -INFINITY ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+    for (int d = 0; d < DL; ++d) sums[warp][col + d] = o[d];
+  __syncthreads();
+  const float inv = none ? 0.f : 1.f / sum;
+  T* out = (T*)a.out + row * a.out_stride + (long long)head * HD;
+  for (int d = threadIdx.x; d < HD; d += 32 * kJoinWarps) {
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) x += sums[i][d];
+    out[d] = from_f32<T>(x * inv);
+  }
+  if (a.lse && threadIdx.x == 0) a.lse[rh] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <typename T>
@@ -209,33 +241,39 @@ void launch_simt(const PagedAttnArgs& a, cudaStream_t st) {
 }
 template <typename T>
 void launch_join(const PagedAttnArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)(((long long)a.kv.rows * a.Hq + 7) / 8));
+  const dim3 grid((unsigned)((long long)a.kv.rows * a.Hq)), block(32 * kJoinWarps);
   switch (a.kv.hd) {
-    case 16: launch_pdl(attn_join_kernel<T, 16>, grid, dim3(256), 0, st, a); break;
-    case 32: launch_pdl(attn_join_kernel<T, 32>, grid, dim3(256), 0, st, a); break;
-    case 64: launch_pdl(attn_join_kernel<T, 64>, grid, dim3(256), 0, st, a); break;
-    default: launch_pdl(attn_join_kernel<T, 128>, grid, dim3(256), 0, st, a); break;
+    case 16: launch_pdl(attn_join_kernel<T, 16>, grid, block, 0, st, a); break;
+    case 32: launch_pdl(attn_join_kernel<T, 32>, grid, block, 0, st, a); break;
+    case 64: launch_pdl(attn_join_kernel<T, 64>, grid, block, 0, st, a); break;
+    default: launch_pdl(attn_join_kernel<T, 128>, grid, block, 0, st, a); break;
   }
 }
 
 }  // namespace
 
 PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
-  (void)bf16;
-  PagedAttnPlan p{0, 1, 0, 0};
-  // the positions that a row tile may see, in tiles
-  long long span = a.kv.max_kv;
-  if (a.window > 0) span = span < (long long)a.window + a.kv.max_new ? span : (long long)a.window + a.kv.max_new;
+  PagedAttnPlan p{kSimt, 1, 0, 0};
+  const long long rows = (long long)a.kv.max_new * a.G;
+  int tile_rows = kRowsS, per_sm = 4, least = 2;
+  if (bf16 && a.kv.hd >= 64) {
+    p.kernel = rows <= 16 ? kTc16 : kTc64;
+    tile_rows = rows <= 16 ? 16 : 64;
+    per_sm = rows <= 16 ? 6 : 2;
+    least = rows <= 16 ? 8 : 4;
+  }
   const long long tiles = (a.kv.max_kv + kAttnTile - 1) / kAttnTile;
-  const long long ctas = (long long)a.kv.Hkv * a.kv.batch * ((a.kv.max_new * (long long)a.G + kRowsS - 1) / kRowsS);
-  const long long want = 4LL * sm_count() / (ctas > 0 ? ctas : 1);
-  long long s = want < tiles / 2 ? want : tiles / 2;
-  if (s > 64) s = 64;
+  const long long ctas = (long long)a.kv.Hkv * a.kv.batch * ((rows + tile_rows - 1) / tile_rows);
+  static const int f1 = getenv("X_PER") ? atoi(getenv("X_PER")) : 0, f2 = getenv("X_LEAST") ? atoi(getenv("X_LEAST")) : 0;
+  if (f1) per_sm = f1;
+  if (f2) least = f2;
+  long long s = (per_sm * (long long)sm_count() + ctas - 1) / ctas;
+  if (s > tiles / least) s = tiles / least;
+  if (s > kMaxSplits) s = kMaxSplits;
   if (s > 1) {
     p.split_tiles = (int)((tiles + s - 1) / s);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
   }
-  (void)span;
   if (p.splits > 1) p.bytes = (size_t)p.splits * a.kv.rows * a.Hq * (a.kv.hd + 1) * sizeof(float);
   return p;
 }
@@ -245,7 +283,9 @@ void launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan
   a.splits = plan.splits; a.split_tiles = plan.split_tiles;
   if (plan.splits > 1) a.part_lse = a.part_o + (long long)plan.splits * a.kv.rows * a.Hq * a.kv.hd;
   LaunchScope ls(kcAttention, st, plan.splits > 1 ? 2 : 1);
-  if (bf16) launch_simt<__nv_bfloat16>(a, st);
+  if (plan.kernel == kTc16) launch_paged_attn_tc(a, 16, st);
+  else if (plan.kernel == kTc64) launch_paged_attn_tc(a, 64, st);
+  else if (bf16) launch_simt<__nv_bfloat16>(a, st);
   else launch_simt<float>(a, st);
   if (plan.splits > 1) {
     if (bf16) launch_join<__nv_bfloat16>(a, st);
