@@ -14,11 +14,12 @@
 namespace nz {
 
 int sm_count();
+bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st);
 void launch_paged_attn_tc(const PagedAttnArgs& a, int rows, cudaStream_t st);
 
 namespace {
 
-enum { kSimt = 0, kTc16 = 1, kTc64 = 2 };
+enum { kSimt = 0, kTc16 = 1, kTc64 = 2, kUmma = 3 };
 constexpr int kMaxSplits = 64;
 constexpr int kRowsS = 16, kPosS = 32, kWarpsS = 4, kRowsWarp = kRowsS / kWarpsS;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -261,6 +262,7 @@ PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
     tile_rows = rows <= 16 ? 16 : 64;
     per_sm = rows <= 16 ? 6 : 2;
     least = rows <= 16 ? 8 : 4;
+    if (rows > 64 && a.kv.page_size % 8 == 0) { p.kernel = kUmma; tile_rows = 256; per_sm = 1; least = 8; }
   }
   const long long tiles = (a.kv.max_kv + kAttnTile - 1) / kAttnTile;
   const long long ctas = (long long)a.kv.Hkv * a.kv.batch * ((rows + tile_rows - 1) / tile_rows);
@@ -271,7 +273,7 @@ PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
   if (s > tiles / least) s = tiles / least;
   if (s > kMaxSplits) s = kMaxSplits;
   if (s > 1) {
-    p.split_tiles = (int)((tiles + s - 1) / s);
+    p.split_tiles = (int)((tiles + s - 1) / s + 1) / 2 * 2;
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
   }
   if (p.splits > 1) p.bytes = (size_t)p.splits * a.kv.rows * a.Hq * (a.kv.hd + 1) * sizeof(float);
@@ -283,8 +285,9 @@ void launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan
   a.splits = plan.splits; a.split_tiles = plan.split_tiles;
   if (plan.splits > 1) a.part_lse = a.part_o + (long long)plan.splits * a.kv.rows * a.Hq * a.kv.hd;
   LaunchScope ls(kcAttention, st, plan.splits > 1 ? 2 : 1);
-  if (plan.kernel == kTc16) launch_paged_attn_tc(a, 16, st);
-  else if (plan.kernel == kTc64) launch_paged_attn_tc(a, 64, st);
+  if (plan.kernel == kUmma && launch_paged_attn_umma(a, st)) {}
+  else if (plan.kernel == kTc16) launch_paged_attn_tc(a, 16, st);
+  else if (plan.kernel >= kTc64) launch_paged_attn_tc(a, 64, st);
   else if (bf16) launch_simt<__nv_bfloat16>(a, st);
   else launch_simt<float>(a, st);
   if (plan.splits > 1) {

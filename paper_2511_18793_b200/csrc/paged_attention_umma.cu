@@ -1,0 +1,473 @@
+// Attention over a paged cache on the Blackwell tensor path (tcgen05 + TMEM, bf16, heads of 64 and 128): calls of many query rows, which are bound by
+// the two products and the exponentials between them.
+//
+// A CTA has one (sequence, KV head), 256 query rows as two tiles A and B of 128 (tokens times the heads of the group), and a share of the context in
+// tiles of 128 positions.  Warp 0 brings K and V tiles into one ring by TMA (a box of 64 columns per page or piece of a page), warp 1 issues the products, warps
+// 4 to 7 and 8 to 11 are the softmax of A and of B, one thread per row (a TMEM lane is a row).  TMEM: S_A, S_B (128 columns each), O_A, O_B.
+//   S_X = Q_X K^T, then the row's scores through registers: running reference maximum (raised only when the true one has grown by more
+//   than 8 in log2, when O is rescaled in TMEM), base-2 exponentials, P as bf16 over the columns that its scores came from;
+//   O_X += P V with P read from TMEM; S_X of the next tile is issued right behind it.
+// While one tile's rows go through softmax, the tensor core runs the other tile's products: P_A V, S_A', P_B V, S_B', ...
+// What a row does not see has no part in its sums (see paged_attention_tc.cu); a thread looks after one position of a tile on the edge.
+// Waits are bounded as everywhere.
+#include <math.h>
+#include <stdlib.h>
+
+#include "gemm_epilogue.cuh"
+#include "paged_attention.cuh"
+
+namespace nz {
+
+namespace {
+
+using namespace gemm_detail;
+using namespace paged_detail;
+
+constexpr int kPosP = 128;         // positions per tile
+constexpr int kThreadsP = 384;     // warps 0 to 3: copies, products, two idle; 4 to 7: rows A; 8 to 11: rows B
+constexpr float kRaise = 8.f;
+
+template <int HD> struct UCfg {
+  static constexpr int kQBytes = 128 * HD * 2;                 // one row tile
+  static constexpr int kTileBytes = kPosP * HD * 2;            // one K or V tile
+  static constexpr int kSlots = HD == 128 ? 5 : 8;
+  static constexpr int kBarBytes = 256;
+  static constexpr int kSmemBytes = 2 * kQBytes + kSlots * kTileBytes + kBarBytes + 1024;
+  static constexpr uint32_t kColO = 256;                       // S_A 0, S_B 128, O_A 256, O_B 256 + HD
+  static constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kPosP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) /* B is N-major */ | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  static_assert(kSmemBytes <= 227 * 1024 && 2 * kSmemBytes > 227 * 1024, "one CTA per SM");
+};
+
+__device__ __forceinline__ void mma_a_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// N-major operand tile with the 128-byte swizzle: 8-row groups along K 1024 B apart, 64-element groups along N `lbo` bytes apart.
+__device__ __forceinline__ uint64_t desc_nmajor(uint32_t addr, uint32_t lbo) {
+  return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)((lbo >> 4) & 0x3FFF) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+template <int HD, bool FORM>
+__global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                                                                      PagedAttnArgs a, int row_tiles, int box_rows) {
+  using C = UCfg<HD>;
+  constexpr int SR = C::kSlots, NH = HD / 64, KS = HD / 16;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t ring = base + 2 * C::kQBytes, bar_base = ring + SR * C::kTileBytes;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (SR + s); };
+  auto s_full = [&](int x) { return bar_base + 8u * (2 * SR + x); };          // S_X of tile j is in TMEM (and O_X holds the tiles before it)
+  auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 2 + x); };      // P_X of tile j is
+  auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 6));
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  volatile uint32_t* odd_flag = tmem_slot + 2;      // a value that is not finite was taken out of a tile
+  static_assert(8 * (2 * SR + 6) + 12 <= C::kBarBytes, "barrier area");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_wait();
+  pdl_launch();
+  AttnCta cta = attn_cta(a, row_tiles);
+  cta.tile = row_tiles - 1 - cta.tile;              // the rows that see the most context go first
+  const int kvh = cta.kvh, b = cta.b;
+  const PagedSeq sq = paged_seq(a.kv, b, kvh == 0 && cta.tile == 0 && cta.split == 0 && threadIdx.x == 0);
+  const int G = a.G, R = sq.n * G, r0 = cta.tile * 256;
+  if (r0 >= R) return;
+  const int first_p = sq.len - sq.n;
+  const bool two = r0 + 128 < R;                    // there are rows B
+  const Visible v0 = visible(a, first_p + r0 / G, sq.len), v1 = visible(a, first_p + min(r0 + 255, R - 1) / G, sq.len);
+  const int u_lo = v0.lo, u_hi = v1.hi, c_lo = v1.lo, c_hi = v0.hi;      // what some of the rows see; what all of them see
+  int t_begin = u_lo / kPosP, t_end = (u_hi + kPosP - 1) / kPosP;
+  if (a.splits > 1) {
+    t_begin = max(t_begin, cta.split * (a.split_tiles / 2));
+    t_end = min(t_end, (cta.split + 1) * (a.split_tiles / 2));
+  }
+  const int NT = max(0, t_end - t_begin);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); }
+    *abort_flag = 0; *odd_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_map(&tmK);
+    tma_prefetch_map(&tmV);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(512));
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  // a softmax thread brings its own query row into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist
+  const int x = warp >= 8 ? 1 : 0;                  // row tile of a softmax thread
+  const int row = (warp & 3) * 32 + lane;           // = the TMEM lane this thread may read
+  bool live = false;
+  int tok = 0, head = 0, pos = 0;
+  Visible vis{0, 0};
+  if (warp >= 4) {
+    live = r0 + x * 128 + row < R;
+    const int rr = live ? r0 + x * 128 + row : r0;
+    tok = sq.row0 + rr / G; head = kvh * G + rr % G; pos = first_p + rr / G;
+    if (live) vis = visible(a, pos, sq.len);
+    const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (long long)tok * a.q_stride + (long long)head * HD);
+#pragma unroll
+    for (int c = 0; c < HD / 8; ++c) {
+      const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(gen_base + x * C::kQBytes + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+    }
+    fence_async();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {
+      // ------------------------------------------------------------------ copies: K_0, V_0, K_1, V_1, ... through one ring
+      const uint32_t leader = elect_one();
+      const int nb = kPosP / box_rows;
+      auto look_up = [&](int tile) { return lane < nb ? page_of(a.kv, b, tile * kPosP + lane * box_rows, box_rows, u_lo, u_hi) : 0; };
+      int page = NT > 0 ? look_up(t_begin) : 0, i = 0, s = 0;
+      uint32_t round = 0;
+      bool ok = true;
+      for (int t = 0; t < NT && ok; ++t) {
+        const int next = t + 1 < NT ? look_up(t_begin + t + 1) : 0;
+        const int p0 = (t_begin + t) * kPosP;
+        for (int kv = 0; kv < 2; ++kv, ++i) {
+          if (!warp_wait_uniform(empty_bar(s), round ^ 1u, abort_flag)) { ok = false; break; }
+          mbar_expect_tx_if(full_bar(s), C::kTileBytes, leader);
+          for (int n = 0; n < nb; ++n) {
+            const int pg = __shfl_sync(0xffffffffu, page, n), y = (p0 + n * box_rows) % a.kv.page_size;
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+              tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y, kvh, pg, full_bar(s), leader);
+          }
+          if (++s == SR) { s = 0; round ^= 1u; }
+        }
+        page = next;
+      }
+      if (!ok && lane == 0) {                        // the copies in flight land before the CTA's memory goes away
+        *abort_flag = 1;
+        for (int j = max(0, i - SR); j < i; ++j) mbar_wait(full_bar(j % SR), (j / SR) & 1);
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------------ products
+      const uint32_t leader = elect_one();
+      bool ok = true;
+      auto slot_ready = [&](int i) { return warp_wait_uniform(full_bar(i % SR), (uint32_t)(i / SR) & 1u, abort_flag); };
+      auto issue_s = [&](int xx, int j) {            // S_X = Q_X K_j^T
+        const uint32_t kt = ring + (2 * j % SR) * C::kTileBytes, qt = base + xx * C::kQBytes;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          tc_mma(tmem_base + 128u * xx, smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
+                 C::kIdescS, ks > 0 ? 1u : 0u, leader);
+      };
+      auto issue_pv = [&](int xx, int j) {           // O_X += P_X V_j
+        const uint32_t vt = ring + ((2 * j + 1) % SR) * C::kTileBytes;
+#pragma unroll
+        for (int ks = 0; ks < kPosP / 16; ++ks)
+          mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + 128u * xx + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
+                     j > 0 || ks > 0 ? 1u : 0u, leader);
+      };
+      if (NT > 0) {
+        ok = slot_ready(0);
+        if (ok) {
+          tc_fence_after();
+          issue_s(0, 0);
+          tc_commit_if(s_full(0), leader);
+          if (two) { issue_s(1, 0); tc_commit_if(s_full(1), leader); }
+          tc_commit_if(empty_bar(0), leader);        // K_0 may be overwritten
+        }
+      }
+      for (int j = 0; j < NT && ok; ++j) {
+        const bool more = j + 1 < NT;
+        if (!slot_ready(2 * j + 1) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
+        for (int xx = 0; xx < (two ? 2 : 1); ++xx) {
+          const bool last = xx == 1 || !two;
+          if (!warp_wait_uniform(p_full(xx), (uint32_t)j & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          issue_pv(xx, j);
+          if (last) tc_commit_if(empty_bar((2 * j + 1) % SR), leader);
+          if (more) {
+            issue_s(xx, j + 1);                      // (behind P_X V_j, whose P lies where this goes: a CTA's products run in order)
+            tc_commit_if(s_full(xx), leader);
+            if (last) tc_commit_if(empty_bar((2 * j + 2) % SR), leader);
+          } else {
+            tc_commit_if(o_full(xx), leader);
+          }
+        }
+      }
+      if (!ok && leader) *abort_flag = 1;
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // ------------------------------------------------------------------ softmax, one thread per row
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem_base + lane_addr + 128u * x, t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
+    const float sc = FORM ? 1.f : a.scale * 1.4426950408889634f;       // scores in base 2 (FORM: they come so)
+    const float slope = FORM && a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
+    const float cap2 = a.softcap * 1.4426950408889634f, inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+    float m_ref = -INFINITY, l_run = 0.f;
+    bool ok = true, edges = false;
+    if (x == 0 || two) {
+      for (int j = 0; j < NT; ++j) {
+        const int p0 = (t_begin + j) * kPosP;
+        const bool edge = p0 < c_lo || p0 + kPosP > c_hi;
+        ok = warp_wait_uniform(s_full(x), (uint32_t)j & 1u, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        float sv[kPosP];
+        {
+          uint32_t r[kPosP];
+#pragma unroll
+          for (int c = 0; c < kPosP / 32; ++c) tmem_ld32_async(t_s + 32u * c, r + 32 * c);
+          tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < kPosP; ++c) { asm volatile("" : "+r"(r[c])); sv[c] = __uint_as_float(r[c]); }
+        }
+        if constexpr (FORM) {
+#pragma unroll
+          for (int c = 0; c < kPosP; ++c) {
+            float v = a.softcap > 0.f ? cap2 * tanh_fast(sv[c] * inv_cap) : sv[c] * (a.scale * 1.4426950408889634f);
+            sv[c] = v - slope * fabsf((float)(pos - (p0 + c)));
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int c = 0; c < kPosP; ++c)
+            if (p0 + c < vis.lo || p0 + c >= vis.hi) sv[c] = -INFINITY;
+        }
+        float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kPosP; c += 8)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + 2 * q], sv[c + 2 * q + 1]);
+        // (a negative scale turns the order round)
+        float mx = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sc;
+        if (sc < 0.f) {
+          mx = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < kPosP; ++c)
+            if (!edge || (p0 + c >= vis.lo && p0 + c < vis.hi)) mx = fmaxf(mx, sv[c] * sc);
+        }
+        const bool raise = mx > m_ref + kRaise || (m_ref == -INFINITY && mx > -INFINITY);
+        const float m_new = raise ? mx : m_ref;
+        const float m_safe = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = raise ? ex2(m_ref - m_safe) : 1.f;
+        m_ref = m_new;
+        if (j > 0 && __any_sync(0xffffffffu, raise)) {      // rescale O (its products so far are complete: S_j was issued behind them)
+#pragma unroll 1
+          for (int c = 0; c < HD / 32; ++c) {
+            uint32_t ov[32];
+            tmem_ld32_async(t_o + 32u * c, ov);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) { asm volatile("" : "+r"(ov[i])); ov[i] = __float_as_uint(__uint_as_float(ov[i]) * corr); }
+            tmem_st16(t_o + 32u * c, ov);
+            tmem_st16(t_o + 32u * c + 16u, ov + 16);
+          }
+        }
+        const f32x2 sc2 = pack2(sc, sc), neg_m2 = pack2(-m_safe, -m_safe);
+        f32x2 rs2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+        for (int h = 0; h < kPosP / 32; ++h) {       // P over the first half of the columns its scores came from
+          uint32_t pk[16];
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            float x0, x1;
+            unpack2(fma2(pack2(sv[32 * h + c], sv[32 * h + c + 1]), sc2, neg_m2), x0, x1);
+            if (edge && sc <= 0.f) {                 // (-inf times a scale of 0 or below)
+              if (sv[32 * h + c] == -INFINITY) x0 = -INFINITY;
+              if (sv[32 * h + c + 1] == -INFINITY) x1 = -INFINITY;
+            }
+            const float e0 = ex2(x0), e1 = ex2(x1);
+            rs2[(c >> 1) & 1] = add2(rs2[(c >> 1) & 1], pack2(e0, e1));
+            const __nv_bfloat162 pb = __floats2bfloat162_rn(e0, e1);
+            pk[c >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
+          }
+          tmem_st16(t_s + 16u * h, pk);
+        }
+        float rs_lo, rs_hi;
+        unpack2(add2(rs2[0], rs2[1]), rs_lo, rs_hi);
+        l_run = l_run * corr + (rs_lo + rs_hi);
+        if (edge) {
+          // this thread's position of the V tile: zeros where no row of the CTA sees it; where some do not, finite values stay
+          edges = true;
+          ok = warp_wait_uniform(full_bar((2 * j + 1) % SR), (uint32_t)((2 * j + 1) / SR) & 1u, abort_flag);
+          if (!ok) break;
+          uint8_t* vg = gen_base + (ring - base) + ((2 * j + 1) % SR) * C::kTileBytes + row * 128;
+          const int p = p0 + row;
+          if (p < u_lo || p >= u_hi) {
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+          } else if (p < c_lo || p >= c_hi) {
+            for (int c = 0; c < HD / 8; ++c) {
+              uint4* at = reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4));
+              uint4 v = *at;
+              uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+              bool odd = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; odd = true; }
+                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; odd = true; }
+              }
+              if (odd) { *at = v; *odd_flag = 1; }
+            }
+          }
+          fence_async();
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(x));
+      }
+      if (ok && NT > 0) {
+        ok = warp_wait_uniform(o_full(x), 0u, abort_flag);
+        tc_fence_after();
+      }
+    }
+    if (!ok && lane == 0) *abort_flag = 1;
+    // (a wait that gave up leaves the others of the CTA to theirs: all softmax warps come here)
+    asm volatile("barrier.sync.aligned 1, 256;" ::: "memory");
+    if (!*abort_flag && (x == 0 || two)) {
+      const bool odd = edges && *odd_flag, none = l_run == 0.f;
+      const float inv = none ? 0.f : 1.f / l_run;
+      const long long at = ((long long)cta.split * a.kv.rows + tok) * a.Hq + head;
+#pragma unroll 1
+      for (int c = 0; c < HD / 32; ++c) {
+        float ov[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) ov[i] = 0.f;
+        if (NT > 0) tmem_ld32(t_o + 32u * c, ov);    // warp-collective: rows that do not exist take part
+        if (odd) {
+          // the values that were taken out, to the rows that see them
+          for (int p = max(u_lo, t_begin * kPosP); p < min(u_hi, t_end * kPosP); ++p) {
+            if (p >= c_lo && p < c_hi) { p = c_hi - 1; continue; }
+            const int page = page_of(a.kv, b, p, 1, u_lo, u_hi);
+            if (page >= a.kv.n_pages || p < vis.lo || p >= vis.hi) continue;
+            const __nv_bfloat16* v = (const __nv_bfloat16*)a.kv.v + page * a.kv.page_stride + kvh * a.kv.head_stride + (long long)(p % a.kv.page_size) * a.kv.pos_stride + 32 * c;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float y = __bfloat162float(v[i]);
+              if (!(fabsf(y) < INFINITY)) ov[i] += y;
+            }
+          }
+          __syncwarp();
+        }
+        if (live) {
+          if (none) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) ov[i] = 0.f;
+          }
+          if (a.splits > 1) {
+            float4* op = reinterpret_cast<float4*>(a.part_o + at * HD + 32 * c);
+            if (!none)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) op[i] = make_float4(ov[4 * i] * inv, ov[4 * i + 1] * inv, ov[4 * i + 2] * inv, ov[4 * i + 3] * inv);
+          } else {
+            uint4* op = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + (long long)tok * a.out_stride + (long long)head * HD + 32 * c);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const uint2 lo = pack_bf16x4(ov[8 * u] * inv, ov[8 * u + 1] * inv, ov[8 * u + 2] * inv, ov[8 * u + 3] * inv);
+              const uint2 hi = pack_bf16x4(ov[8 * u + 4] * inv, ov[8 * u + 5] * inv, ov[8 * u + 6] * inv, ov[8 * u + 7] * inv);
+              op[u] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            }
+          }
+        }
+        __syncwarp();
+      }
+      if (live) {
+        const float lse2 = none ? -INFINITY : m_ref + log2f(l_run);
+        if (a.splits > 1) a.part_lse[at] = lse2;
+        else if (a.lse) a.lse[(long long)tok * a.Hq + head] = lse2 * 0.6931471805599453f;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512));
+  }
+  if (threadIdx.x == 0 && *abort_flag) atomicOr(a.kv.status, kStInternal);
+}
+
+// The softmax warpgroups take 224 registers a thread and leave 56 to the other: the launch has to have had 168 for all (else the kernel would wait).
+template <int HD, bool FORM>
+bool registers_add_up() {
+  cudaFuncAttributes at{};
+  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM>) == cudaSuccess && at.numRegs * kThreadsP >= 56 * 128 + 224 * 256;
+}
+
+template <int HD, bool FORM>
+bool launch(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, int box_rows, cudaStream_t st) {
+  using C = UCfg<HD>;
+  static const bool fits = registers_add_up<HD, FORM>();
+  if (!fits) return false;
+  static PerDeviceOnce configured;
+  configured.run([] { cudaFuncSetAttribute(paged_attn_umma_kernel<HD, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes); });
+  const int row_tiles = (int)(((long long)a.kv.max_new * a.G + 255) / 256);
+  launch_pdl(paged_attn_umma_kernel<HD, FORM>, dim3((unsigned)((long long)a.kv.Hkv * row_tiles * a.splits * a.kv.batch)), dim3(kThreadsP), C::kSmemBytes, st, tk, tv, a,
+             row_tiles, box_rows);
+  return true;
+}
+
+}  // namespace
+
+// false: not launched (no tensor map).
+bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
+  CUtensorMap tk{}, tv{};
+  const int box = paged_box_rows(a.kv.page_size);
+  if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
+  const bool form = a.softcap > 0.f || a.slopes;
+  if (a.kv.hd == 64) return form ? launch<64, true>(a, tk, tv, box, st) : launch<64, false>(a, tk, tv, box, st);
+  return form ? launch<128, true>(a, tk, tv, box, st) : launch<128, false>(a, tk, tv, box, st);
+}
+
+}  // namespace nz
