@@ -5,7 +5,6 @@ this module fails loudly when the library has not been built (there is no fallba
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import math
 import os
@@ -201,11 +200,12 @@ class Rope:
                          self.turns_fast, self.turns_slow, self.magnitude)
 
 
-@dataclass
 class RopeTable:
     """What Engine.rope_table returns: the cosines and sines of positions 0 .. n - 1, float32 [n, rot_dim]."""
-    rope: Rope
-    table: torch.Tensor
+
+    def __init__(self, rope: Rope, table: torch.Tensor):
+        self.rope, self.table = rope, table
+        self._ref = C.byref(rope.struct())
 
 
 class PagedKV:
@@ -230,15 +230,19 @@ class PagedKV:
             assert t.device == k_pool.device and t.is_cuda
         self.k_pool, self.v_pool, self.page_table, self.row_start, self.kv_len = k_pool, v_pool, page_table, row_start, kv_len
         n_pages, heads, page_size, hd = k_pool.shape
+        self._heads, self._hd, self._dtype = heads, hd, k_pool.dtype
+        self._need: Dict[tuple, int] = {}          # workspace bytes by the sizes of a call
         self.max_new, self.max_kv = max_new, max_pages * page_size if max_kv is None else max_kv
         st = k_pool.stride()
         self._s = NezhaPagedKV(k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
                                max(page_table.stride(0), max_pages), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr(), 0, 0, self.max_kv)
+        self._ref = C.byref(self._s)
 
-    def struct(self, rows: int) -> NezhaPagedKV:
+    def _for(self, rows: int):
+        """The C struct for a call of `rows` rows."""
         self._s.rows = rows
-        self._s.max_new = rows if self.max_new is None else min(self.max_new, rows)
-        return self._s
+        self._s.max_new = rows if self.max_new is None or self.max_new > rows else self.max_new
+        return self._ref
 
 
 class Engine:
@@ -275,6 +279,9 @@ class Engine:
         if st != 0:
             raise NezhaError(st, "nezha_create failed")
         self.batch = 0
+        self._dtype = torch.bfloat16 if cfg.dtype == 1 else torch.float32
+        self._dev = self.arena.get_device()
+        self._raw_stream = self._stream_ptr() or 0
 
     def _stream_ptr(self):
         return None if self.stream is None else self.stream.cuda_stream
@@ -438,49 +445,52 @@ class Engine:
         return C_out
 
     # -- operators over a paged context cache, 8-bit projections --------------------------------------------
+    # (A call's launch takes 3 us; these methods look at each tensor once and make no object that they do not need.)
     @property
     def dtype(self) -> torch.dtype:
-        return torch.bfloat16 if self.cfg.dtype == 1 else torch.float32
+        return self._dtype
 
-    def _on_stream(self):
-        """Buffers that a method makes belong to the engine's stream, whatever stream is current."""
-        mine = torch.cuda.default_stream(self.arena.device) if self.stream is None else self.stream
-        return contextlib.nullcontext() if torch.cuda.current_stream(self.arena.device) == mine else torch.cuda.stream(mine)
+    def _new(self, shape, dtype: torch.dtype) -> torch.Tensor:
+        """A buffer that belongs to the engine's stream, whatever stream is current."""
+        if torch._C._cuda_getCurrentRawStream(self._dev) == self._raw_stream:
+            return torch.empty(shape, dtype=dtype, device=self.arena.device)
+        with torch.cuda.stream(torch.cuda.default_stream(self.arena.device) if self.stream is None else self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.arena.device)
 
-    def _rows(self, t: torch.Tensor, heads: Optional[int], hd: int, rows: Optional[int]) -> Tuple[int, int]:
-        """(pointer, row stride) of [rows, heads, hd] whose heads lie side by side."""
-        assert t.dim() == 3 and t.shape[2] == hd and (heads is None or t.shape[1] == heads) and (rows is None or t.shape[0] == rows)
-        assert t.dtype == self.dtype and t.device == self.arena.device
-        assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == hd)
-        return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * hd)
+    def _rows(self, t: torch.Tensor, heads: int, hd: int, rows: int) -> int:
+        """Row stride of [rows, heads, hd] whose heads lie side by side."""
+        st = t.stride()
+        assert t.shape == (rows, heads, hd) and t.dtype is self._dtype and t.get_device() == self._dev
+        assert st[2] == 1 and (st[1] == hd or heads == 1)
+        return st[0] if rows > 1 else max(st[0], heads * hd)
 
     def rope_table(self, rope: Rope, n_positions: int) -> RopeTable:
-        with self._on_stream():
-            table = torch.empty(n_positions, rope.rot_dim, dtype=torch.float32, device=self.arena.device)
-        self._check(lib.nezha_rope_table(self._h, C.byref(rope.struct()), table.data_ptr(), n_positions))
-        return RopeTable(rope, table)
+        out = RopeTable(rope, self._new((n_positions, rope.rot_dim), torch.float32))
+        self._check(lib.nezha_rope_table(self._h, out._ref, out.table.data_ptr(), n_positions))
+        return out
 
     def kv_append(self, kv: PagedKV, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, rope: Optional[RopeTable] = None,
                   positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """k, v [rows, n_kv_heads, head_dim] (and q [rows, n_q_heads, head_dim]) of the new rows, e.g. slices of a fused QKV product.
         Returns the rotated q (q_out, a new tensor if not given; q itself is legal)."""
-        _, heads, _, hd = kv.k_pool.shape
-        rows = int(k.shape[0])
-        assert kv.k_pool.dtype == self.dtype
-        kp, ks = self._rows(k, heads, hd, None)
-        vp, vs = self._rows(v, heads, hd, rows)
-        qp = qs = op = os_ = None
+        heads, hd, rows = kv._heads, kv._hd, k.shape[0]
+        assert kv._dtype is self._dtype
+        ks, vs = self._rows(k, heads, hd, rows), self._rows(v, heads, hd, rows)
+        qp = op = None
+        qs = os_ = hq = 0
         if q is not None:
-            qp, qs = self._rows(q, None, hd, rows)
+            hq = q.shape[1]
+            qs, qp = self._rows(q, hq, hd, rows), q.data_ptr()
             if q_out is None:
-                with self._on_stream():
-                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            op, os_ = self._rows(q_out, q.shape[1], hd, rows)
+                q_out = self._new((rows, hq, hd), q.dtype)
+            os_, op = self._rows(q_out, hq, hd, rows), q_out.data_ptr()
         assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == rows)
-        table = None if rope is None else rope.table
-        st = lib.nezha_kv_append(self._h, C.byref(kv.struct(rows)), qp, qs or 0, 0 if q is None else q.shape[1], op, os_ or 0, kp, ks, vp, vs,
-                                 None if rope is None else C.byref(rope.rope.struct()), _ptr(table), 0 if table is None else table.shape[0],
-                                 _ptr(positions))
+        ref = tab = None
+        n_table = 0
+        if rope is not None:
+            ref, tab, n_table = rope._ref, rope.table.data_ptr(), rope.table.shape[0]
+        st = lib.nezha_kv_append(self._h, kv._for(rows), qp, qs, hq, op, os_, k.data_ptr(), ks, v.data_ptr(), vs, ref, tab, n_table,
+                                 None if positions is None else _ptr(positions))
         if st:
             self._check(st)
         return q_out
@@ -491,22 +501,30 @@ class Engine:
         """Attention of the new rows q [rows, n_q_heads, head_dim] over their sequences' positions; scale: 1 / sqrt(head_dim) if not given;
         lse: float32 [rows, n_q_heads] to fill.  The workspace, where one is needed, is a new tensor of the call."""
         rows, heads, hd = q.shape
-        assert hd == kv.k_pool.shape[3] and kv.k_pool.dtype == self.dtype
-        qp, qs = self._rows(q, None, hd, None)
-        assert slopes is None or (slopes.dtype == torch.float32 and slopes.numel() == heads)
+        assert hd == kv._hd and kv._dtype is self._dtype
+        qs = self._rows(q, heads, hd, rows)
+        sl = None
+        if slopes is not None:
+            assert slopes.dtype == torch.float32 and slopes.numel() == heads
+            sl = _ptr(slopes)
         assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (rows, heads))
-        form = NezhaAttnForm(int(causal), window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, _ptr(slopes))
-        s = kv.struct(rows)
-        need = lib.nezha_paged_attention_workspace(self._h, C.byref(s), heads, C.byref(form))
-        ws = None
-        if out is None or need:
-            with self._on_stream():
-                if out is None:
-                    out = torch.empty(rows, heads, hd, dtype=q.dtype, device=q.device)
-                if need:
-                    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-        op, os_ = self._rows(out, heads, hd, rows)
-        st = lib.nezha_paged_attention(self._h, C.byref(s), qp, qs, heads, C.byref(form), op, os_, _ptr(lse), _ptr(ws), need)
+        form = C.byref(NezhaAttnForm(1 if causal else 0, window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl))
+        ref = kv._for(rows)
+        key = (rows, heads, kv.max_new, kv.max_kv, causal, window)
+        need = kv._need.get(key)
+        if need is None:
+            need = lib.nezha_paged_attention_workspace(self._h, ref, heads, form)
+            if len(kv._need) > 64:
+                kv._need.clear()
+            kv._need[key] = need
+        if out is None:
+            out = self._new((rows, heads, hd), q.dtype)
+        ws = wp = None
+        if need:
+            ws = self._new((need,), torch.uint8)
+            wp = ws.data_ptr()
+        st = lib.nezha_paged_attention(self._h, ref, q.data_ptr(), qs, heads, form, out.data_ptr(), self._rows(out, heads, hd, rows),
+                                       None if lse is None else _ptr(lse), wp, need)
         if st:
             self._check(st)
         return out
@@ -514,13 +532,14 @@ class Engine:
     def quantize_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """x [M, K] -> (int8 [M, K], float32 [M]); rows of x may be strided."""
         M, K = x.shape
-        assert x.dtype == self.dtype and x.device == self.arena.device and (x.stride(1) == 1 or K == 1)
-        if q is None or scale is None:
-            with self._on_stream():
-                q = torch.empty(M, K, dtype=torch.int8, device=x.device) if q is None else q
-                scale = torch.empty(M, dtype=torch.float32, device=x.device) if scale is None else scale
-        assert q.dtype == torch.int8 and tuple(q.shape) == (M, K) and scale.dtype == torch.float32 and scale.numel() == M
-        st = lib.nezha_quantize_rows(self._h, x.data_ptr(), x.stride(0) if M > 1 else max(x.stride(0), K), M, K, _ptr(q), _ptr(scale))
+        xs = x.stride()
+        assert x.dtype is self._dtype and x.get_device() == self._dev and (xs[1] == 1 or K == 1)
+        if q is None:
+            q = self._new((M, K), torch.int8)
+        if scale is None:
+            scale = self._new((M,), torch.float32)
+        assert q.dtype is torch.int8 and q.shape == (M, K) and scale.dtype is torch.float32 and scale.numel() == M
+        st = lib.nezha_quantize_rows(self._h, x.data_ptr(), xs[0] if M > 1 else max(xs[0], K), M, K, _ptr(q), _ptr(scale))
         if st:
             self._check(st)
         return q, scale
@@ -529,10 +548,10 @@ class Engine:
                   bias: Optional[torch.Tensor] = None) -> torch.Tensor:
         M, K = A.shape
         N = W.shape[0]
-        assert A.dtype == W.dtype == torch.int8 and W.shape[1] == K and tuple(C_out.shape) == (M, N)
-        assert C_out.dtype == (self.dtype if epilogue == 0 else torch.float32)
-        assert a_scale.dtype == w_scale.dtype == torch.float32 and a_scale.numel() == M and w_scale.numel() == N
-        assert bias is None or (bias.dtype == torch.float32 and bias.numel() == N)
+        assert A.dtype is torch.int8 and W.dtype is torch.int8 and W.shape[1] == K and C_out.shape == (M, N)
+        assert C_out.dtype is (self._dtype if epilogue == 0 else torch.float32)
+        assert a_scale.dtype is torch.float32 and w_scale.dtype is torch.float32 and a_scale.numel() == M and w_scale.numel() == N
+        assert bias is None or (bias.dtype is torch.float32 and bias.numel() == N)
         st = lib.nezha_gemm_int8(self._h, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(C_out), M, N, K, epilogue, _ptr(bias))
         if st:
             self._check(st)

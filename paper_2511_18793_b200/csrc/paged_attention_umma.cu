@@ -91,7 +91,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <int HD, bool FORM>
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// tanh(y) / y as a polynomial in y^2, |y| <= 0.6: fitted to tanh for the least relative error, 8e-8.
+constexpr float kTanhRange = 0.6f;
+constexpr float kTanh[5] = {0.99999994f, -0.33332309f, 0.13310173f, -0.052101482f, 0.015475428f};
+
+// FORM, a sum of: scores capped; scores biased by their distance (or a scale that is not positive).  0: neither.
+enum { kCap = 1, kBias = 2 };
+
+template <int HD, int FORM>
 __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                                                                       PagedAttnArgs a, int row_tiles, int box_rows) {
   using C = UCfg<HD>;
@@ -105,10 +118,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   auto s_full = [&](int x) { return bar_base + 8u * (2 * SR + x); };          // S_X of tile j is in TMEM (and O_X holds the tiles before it)
   auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 2 + x); };      // P_X of tile j is
   auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 6));
+  auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 6 + x); };      // its first 64 positions are
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 8));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   volatile uint32_t* odd_flag = tmem_slot + 2;      // a value that is not finite was taken out of a tile
-  static_assert(8 * (2 * SR + 6) + 12 <= C::kBarBytes, "barrier area");
+  static_assert(8 * (2 * SR + 8) + 12 <= C::kBarBytes, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_wait();
@@ -132,7 +146,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); }
+    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); }
     *abort_flag = 0; *odd_flag = 0;
     mbar_fence_init();
     tma_prefetch_map(&tmK);
@@ -208,12 +222,14 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
           tc_mma(tmem_base + 128u * xx, smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
                  C::kIdescS, ks > 0 ? 1u : 0u, leader);
       };
-      auto issue_pv = [&](int xx, int j) {           // O_X += P_X V_j
+      auto issue_pv = [&](int xx, int j, int half) {      // O_X += P_X V_j, 64 of the positions
         const uint32_t vt = ring + ((2 * j + 1) % SR) * C::kTileBytes;
 #pragma unroll
-        for (int ks = 0; ks < kPosP / 16; ++ks)
+        for (int kk = 0; kk < kPosP / 32; ++kk) {
+          const int ks = half * (kPosP / 32) + kk;
           mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + 128u * xx + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
                      j > 0 || ks > 0 ? 1u : 0u, leader);
+        }
       };
       if (NT > 0) {
         ok = slot_ready(0);
@@ -230,9 +246,12 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         if (!slot_ready(2 * j + 1) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
         for (int xx = 0; xx < (two ? 2 : 1); ++xx) {
           const bool last = xx == 1 || !two;
+          if (!warp_wait_uniform(p_half(xx), (uint32_t)j & 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          issue_pv(xx, j, 0);
           if (!warp_wait_uniform(p_full(xx), (uint32_t)j & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          issue_pv(xx, j);
+          issue_pv(xx, j, 1);
           if (last) tc_commit_if(empty_bar((2 * j + 1) % SR), leader);
           if (more) {
             issue_s(xx, j + 1);                      // (behind P_X V_j, whose P lies where this goes: a CTA's products run in order)
@@ -250,15 +269,19 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
     // ------------------------------------------------------------------ softmax, one thread per row
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem_base + lane_addr + 128u * x, t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
-    const float sc = FORM ? 1.f : a.scale * 1.4426950408889634f;       // scores in base 2 (FORM: they come so)
-    const float slope = FORM && a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
-    const float cap2 = a.softcap * 1.4426950408889634f, inv_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+    const float sc = a.scale * 1.4426950408889634f;       // scores in base 2
+    const float slope = (FORM & kBias) && a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
+    // capped: cap2 tanh(s inv_cap) = s (k_0 + k_1 s^2 + ...) while no score of the warp's rows is beyond kTanhRange
+    const float cap2 = (FORM & kCap) ? a.softcap * 1.4426950408889634f : 0.f, inv_cap = (FORM & kCap) ? a.scale / a.softcap : 0.f;
+    const int pos_min = (FORM & kBias) ? __reduce_min_sync(0xffffffffu, pos) : 0;
+    // tiles [j_lo, j_hi) are seen whole by all rows of the CTA
+    const int j_lo = (c_lo + kPosP - 1) / kPosP - t_begin, j_hi = c_hi / kPosP - t_begin;
     float m_ref = -INFINITY, l_run = 0.f;
     bool ok = true, edges = false;
     if (x == 0 || two) {
       for (int j = 0; j < NT; ++j) {
         const int p0 = (t_begin + j) * kPosP;
-        const bool edge = p0 < c_lo || p0 + kPosP > c_hi;
+        const bool edge = j < j_lo || j >= j_hi;
         ok = warp_wait_uniform(s_full(x), (uint32_t)j & 1u, abort_flag);
         if (!ok) break;
         tc_fence_after();
@@ -271,11 +294,42 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 #pragma unroll
           for (int c = 0; c < kPosP; ++c) { asm volatile("" : "+r"(r[c])); sv[c] = __uint_as_float(r[c]); }
         }
-        if constexpr (FORM) {
+        if constexpr ((FORM & kCap) != 0) {
+          float mb[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kPosP; ++c) {
-            float v = a.softcap > 0.f ? cap2 * tanh_fast(sv[c] * inv_cap) : sv[c] * (a.scale * 1.4426950408889634f);
-            sv[c] = v - slope * fabsf((float)(pos - (p0 + c)));
+          for (int c = 0; c < kPosP; c += 4)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mb[q] = fmaxf(mb[q], fabsf(sv[c + q]));
+          // (positions that nobody sees may be beyond; a NaN among them is not noticed here and stays one below)
+          if (__all_sync(0xffffffffu, fmaxf(fmaxf(mb[0], mb[1]), fmaxf(mb[2], mb[3])) * fabsf(inv_cap) <= kTanhRange)) {
+            const float i2 = inv_cap * inv_cap, lead = cap2 * inv_cap;
+            const f32x2 k0 = pack2(kTanh[0] * lead, kTanh[0] * lead), i22 = pack2(i2, i2);
+            const f32x2 k1 = pack2(kTanh[1] * lead, kTanh[1] * lead), k2 = pack2(kTanh[2] * lead, kTanh[2] * lead);
+            const f32x2 k3 = pack2(kTanh[3] * lead, kTanh[3] * lead), k4 = pack2(kTanh[4] * lead, kTanh[4] * lead);
+#pragma unroll
+            for (int c = 0; c < kPosP; c += 2) {
+              const f32x2 v = pack2(sv[c], sv[c + 1]), z = mul2(mul2(v, v), i22);
+              unpack2(mul2(v, fma2(z, fma2(z, fma2(z, fma2(z, k4, k3), k2), k1), k0)), sv[c], sv[c + 1]);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < kPosP; ++c) sv[c] = cap2 * tanh_fast(sv[c] * inv_cap);
+          }
+        } else if constexpr (FORM != 0) {
+          const f32x2 sc2 = pack2(sc, sc);
+#pragma unroll
+          for (int c = 0; c < kPosP; c += 2) unpack2(mul2(pack2(sv[c], sv[c + 1]), sc2), sv[c], sv[c + 1]);
+        }
+        float bias = 0.f;                            // of the whole row: its scores are off by it until the exponential
+        if constexpr ((FORM & kBias) != 0) {
+          const float rel = (float)(pos - p0);
+          if (a.causal || p0 + kPosP - 1 <= pos_min) {
+            bias = -slope * rel;
+#pragma unroll
+            for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(slope, (float)c, sv[c]);
+          } else {
+#pragma unroll
+            for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(-slope, fabsf(rel - (float)c), sv[c]);
           }
         }
         if (edge) {
@@ -288,14 +342,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         for (int c = 0; c < kPosP; c += 8)
 #pragma unroll
           for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + 2 * q], sv[c + 2 * q + 1]);
-        // (a negative scale turns the order round)
-        float mx = max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sc;
-        if (sc < 0.f) {
-          mx = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < kPosP; ++c)
-            if (!edge || (p0 + c >= vis.lo && p0 + c < vis.hi)) mx = fmaxf(mx, sv[c] * sc);
-        }
+        const float mx = FORM ? max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) + bias : max3(fmaxf(mq[0], mq[1]), mq[2], mq[3]) * sc;
         const bool raise = mx > m_ref + kRaise || (m_ref == -INFINITY && mx > -INFINITY);
         const float m_new = raise ? mx : m_ref;
         const float m_safe = m_new == -INFINITY ? 0.f : m_new;
@@ -313,29 +360,6 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             tmem_st16(t_o + 32u * c + 16u, ov + 16);
           }
         }
-        const f32x2 sc2 = pack2(sc, sc), neg_m2 = pack2(-m_safe, -m_safe);
-        f32x2 rs2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-#pragma unroll
-        for (int h = 0; h < kPosP / 32; ++h) {       // P over the first half of the columns its scores came from
-          uint32_t pk[16];
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            float x0, x1;
-            unpack2(fma2(pack2(sv[32 * h + c], sv[32 * h + c + 1]), sc2, neg_m2), x0, x1);
-            if (edge && sc <= 0.f) {                 // (-inf times a scale of 0 or below)
-              if (sv[32 * h + c] == -INFINITY) x0 = -INFINITY;
-              if (sv[32 * h + c + 1] == -INFINITY) x1 = -INFINITY;
-            }
-            const float e0 = ex2(x0), e1 = ex2(x1);
-            rs2[(c >> 1) & 1] = add2(rs2[(c >> 1) & 1], pack2(e0, e1));
-            const __nv_bfloat162 pb = __floats2bfloat162_rn(e0, e1);
-            pk[c >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
-          }
-          tmem_st16(t_s + 16u * h, pk);
-        }
-        float rs_lo, rs_hi;
-        unpack2(add2(rs2[0], rs2[1]), rs_lo, rs_hi);
-        l_run = l_run * corr + (rs_lo + rs_hi);
         if (edge) {
           // this thread's position of the V tile: zeros where no row of the CTA sees it; where some do not, finite values stay
           edges = true;
@@ -362,6 +386,32 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
           }
           fence_async();
         }
+        const f32x2 sc2 = pack2(sc, sc), neg_m2 = pack2(bias - m_safe, bias - m_safe);
+        f32x2 rs2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+        for (int h = 0; h < kPosP / 32; ++h) {       // P over the first half of the columns its scores came from
+          uint32_t pk[16];
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            float x0, x1;
+            const f32x2 v = pack2(sv[32 * h + c], sv[32 * h + c + 1]);
+            unpack2(FORM ? add2(v, neg_m2) : fma2(v, sc2, neg_m2), x0, x1);
+            const float e0 = ex2(x0), e1 = ex2(x1);
+            rs2[(c >> 1) & 1] = add2(rs2[(c >> 1) & 1], pack2(e0, e1));
+            const __nv_bfloat162 pb = __floats2bfloat162_rn(e0, e1);
+            pk[c >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
+          }
+          tmem_st16(t_s + 16u * h, pk);
+          if (h == kPosP / 64 - 1) {                 // half of P is there: its product may begin
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_half(x));
+          }
+        }
+        float rs_lo, rs_hi;
+        unpack2(add2(rs2[0], rs2[1]), rs_lo, rs_hi);
+        l_run = l_run * corr + (rs_lo + rs_hi);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -438,14 +488,14 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   if (threadIdx.x == 0 && *abort_flag) atomicOr(a.kv.status, kStInternal);
 }
 
-// The softmax warpgroups take 224 registers a thread and leave 56 to the other: the launch has to have had 168 for all (else the kernel would wait).
-template <int HD, bool FORM>
+// The softmax warpgroups take 224 registers a thread and leave 56 to the other: the launch has to have 168 for all (else they would wait).
+template <int HD, int FORM>
 bool registers_add_up() {
   cudaFuncAttributes at{};
   return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM>) == cudaSuccess && at.numRegs * kThreadsP >= 56 * 128 + 224 * 256;
 }
 
-template <int HD, bool FORM>
+template <int HD, int FORM>
 bool launch(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, int box_rows, cudaStream_t st) {
   using C = UCfg<HD>;
   static const bool fits = registers_add_up<HD, FORM>();
@@ -458,6 +508,16 @@ bool launch(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv
   return true;
 }
 
+template <int HD>
+bool launch_form(const PagedAttnArgs& a, int form, const CUtensorMap& tk, const CUtensorMap& tv, int box, cudaStream_t st) {
+  switch (form) {
+    case 0: return launch<HD, 0>(a, tk, tv, box, st);
+    case kCap: return launch<HD, kCap>(a, tk, tv, box, st);
+    case kBias: return launch<HD, kBias>(a, tk, tv, box, st);
+    default: return launch<HD, kCap + kBias>(a, tk, tv, box, st);
+  }
+}
+
 }  // namespace
 
 // false: not launched (no tensor map).
@@ -465,9 +525,9 @@ bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
   CUtensorMap tk{}, tv{};
   const int box = paged_box_rows(a.kv.page_size);
   if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
-  const bool form = a.softcap > 0.f || a.slopes;
-  if (a.kv.hd == 64) return form ? launch<64, true>(a, tk, tv, box, st) : launch<64, false>(a, tk, tv, box, st);
-  return form ? launch<128, true>(a, tk, tv, box, st) : launch<128, false>(a, tk, tv, box, st);
+  const int form = (a.softcap > 0.f ? kCap : 0) + (a.slopes || !(a.scale > 0.f) ? kBias : 0);
+  if (a.kv.hd == 64) return launch_form<64>(a, form, tk, tv, box, st);
+  return launch_form<128>(a, form, tk, tv, box, st);
 }
 
 }  // namespace nz
