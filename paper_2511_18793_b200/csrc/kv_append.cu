@@ -2,9 +2,9 @@
 //
 //   (x_a, x_b) -> (x_a cos - x_b sin, x_b cos + x_a sin), pairs (i, i + rot / 2) or (2 i, 2 i + 1) of the first `rot` dimensions
 //
-// Nothing is computed to speak of: the launch reads q, k and v once and writes them once.  A block takes R rows whole (all heads of q, k and v), a
-// thread the same 16-byte chunks of each, so the loads of R rows are in flight while the rows' places are looked up: which
-// sequence a row is of (a 32-way search of row_start by one warp per row), its position, page and table row.
+// Nothing is computed to speak of: the launch reads q, k and v once and writes them once.  A block takes whole rows (all heads of q, k and v), whose
+// loads are in flight while the rows' places are looked up: which sequence a row is of (a 32-way search of row_start by one
+// warp per row), its position, page and table row.
 #include "operators.cuh"
 
 namespace nz {
@@ -78,103 +78,91 @@ __device__ __forceinline__ void look_over(const PagedView& kv) {
     for (int b = threadIdx.x; b < kv.batch; b += blockDim.x) paged_seq(kv, b, true);
 }
 
-// A thread's work on a row: which of q, k and v, the element offset inside the source row and behind the destination's start, the second chunk of a
-// rotated pair of halves, and its columns of the table.
-struct Unit { int kind; long long src, dst; int second, col; };   // kind 0: q, 1: k, 2: v; second 0: one chunk; col -1: copied
+// A row takes `units` x `lanes` threads: a thread has one unit of a head's columns (16 bytes, or the two pieces of a pair of halves) in every
+// `lanes`-th head of q, then k, then v, so that it reads its cosines and sines once per row and its loads of up to kHeads heads are under way together.
+// (A thread per piece of one head, its table columns read again for each: 120 us for 16,008 rows of 32 + 8 + 8 heads of 128.)
+constexpr int kHeads = 6;
 
-// Units of a head: the chunks that are rotated (of the half layout two at a time), then those that are copied.
-template <int N, bool HALVES>
-__device__ __forceinline__ Unit unit_of(const AppendArgs& a, int u, int per_turned, int per_copied) {
-  const int hd = a.kv.hd;
-  Unit r{};
-  int head, w;
-  const int n_turned = (a.Hq + a.kv.Hkv) * per_turned;
-  if (u < n_turned) {
-    head = u / per_turned; w = u - head * per_turned;
-    const int turned = HALVES ? a.rot / 2 / N : a.rot / N;
-    if (w < turned) { r.second = HALVES ? a.rot / 2 : 0; r.col = HALVES ? w * N : w * (N / 2); w *= N; }
-    else { r.col = -1; w = a.rot + (w - turned) * N; }
-    r.kind = head < a.Hq ? 0 : 1;
-    if (r.kind) head -= a.Hq;
-  } else {
-    u -= n_turned;
-    head = u / per_copied; w = (u - head * per_copied) * N;
-    r.kind = 2; r.col = -1;
-  }
-  r.src = (long long)head * hd + w;
-  r.dst = r.kind == 0 ? r.src : (long long)head * a.kv.head_stride + w;
-  return r;
-}
-
-template <typename T, bool HALVES, int R>
-__global__ void kv_append_kernel(AppendArgs a, int units, int per_turned, int per_copied) {
+template <typename T, bool HALVES>
+__global__ void kv_append_kernel(AppendArgs a, int units, int turned, int lanes, int rows_per_block) {
   constexpr int N = Vec<T>::N;
-  __shared__ long long place[R];
-  __shared__ int turn[R];
+  __shared__ long long place[16];
+  __shared__ int turn[16];
   pdl_wait();
   pdl_launch();
-  const int row0 = blockIdx.x * R, warp = threadIdx.x >> 5;
-  const T* const src[3] = {(const T*)a.q, (const T*)a.k, (const T*)a.v};
-  const long long stride[3] = {a.q_stride, a.k_stride, a.v_stride};
+  const int per_row = units * lanes, r = threadIdx.x / per_row, t = threadIdx.x - r * per_row;
+  const int row = blockIdx.x * rows_per_block + r, w = t % units, lane_h = t / units;
+  const bool live = r < rows_per_block && row < a.kv.rows;
+  const int heads = a.Hq + 2 * a.kv.Hkv, hd = a.kv.hd;
+  // the unit's columns: a turned pair of halves, a turned piece, or a piece that is copied
+  const bool turns = w < turned, two = HALVES && turns;
+  const int c0 = turns ? w * N : a.rot + (w - turned) * N, c1 = c0 + a.rot / 2;
+  auto source = [&](int h) {
+    return h < a.Hq ? (const T*)a.q + row * a.q_stride + (long long)h * hd
+                    : h < a.Hq + a.kv.Hkv ? (const T*)a.k + row * a.k_stride + (long long)(h - a.Hq) * hd
+                                          : (const T*)a.v + row * a.v_stride + (long long)(h - a.Hq - a.kv.Hkv) * hd;
+  };
+  float cs[N], sn[N];
+  long long at = -1;
   bool first = true;
-  for (int u = threadIdx.x; u < units || first; u += blockDim.x) {      // (every thread comes through once: the barrier)
-    const bool mine = u < units;
-    Unit t{};
-    uint4 x[R][2];
-    if (mine) {
-      t = unit_of<N, HALVES>(a, u, per_turned, per_copied);
+  for (int h0 = lane_h; first || (live && h0 < heads); h0 += kHeads * lanes) {
+    uint4 x[kHeads][HALVES ? 2 : 1];
+    if (live) {
 #pragma unroll
-      for (int i = 0; i < R; ++i)
-        if (row0 + i < a.kv.rows) {
-          const T* p = src[t.kind] + (row0 + i) * stride[t.kind] + t.src;
-          x[i][0] = *reinterpret_cast<const uint4*>(p);
-          if (HALVES && t.second) x[i][1] = *reinterpret_cast<const uint4*>(p + t.second);
+      for (int i = 0; i < kHeads; ++i)
+        if (h0 + i * lanes < heads) {
+          const T* p = source(h0 + i * lanes);
+          x[i][0] = *reinterpret_cast<const uint4*>(p + c0);
+          if (HALVES && two) x[i][HALVES ? 1 : 0] = *reinterpret_cast<const uint4*>(p + c1);
         }
     }
-    if (first) {
-      for (int i = warp; i < R; i += blockDim.x >> 5) {
-        const RowPlace p = place_of(a, row0 + i);
+    if (first) {                                     // where the rows go, while their loads are on their way
+      for (int i = threadIdx.x >> 5; i < rows_per_block; i += blockDim.x >> 5) {
+        const RowPlace p = place_of(a, blockIdx.x * rows_per_block + i);
         if ((threadIdx.x & 31) == 0) { place[i] = p.place; turn[i] = p.turn; }
       }
       __syncthreads();
       first = false;
-    }
-    if (!mine) break;
+      if (!live || (at = place[r]) < 0) break;
+      if (turns) {
+        const float* tab = a.table + (long long)turn[r] * a.rot + (HALVES ? c0 : c0 / 2);
+        constexpr int P = HALVES ? N : N / 2;        // pairs of the unit
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (place[i] < 0) continue;
-      T* out = t.kind == 0 ? (T*)a.q_out + (row0 + i) * a.q_out_stride : (T*)(t.kind == 1 ? a.kv.k : a.kv.v) + place[i];
-      out += t.dst;
-      if (t.col < 0) { *reinterpret_cast<uint4*>(out) = x[i][0]; continue; }
-      const float* tab = a.table + (long long)turn[i] * a.rot + t.col;
+        for (int c = 0; c < P; c += 2) {
+          const float2 co = *reinterpret_cast<const float2*>(tab + c), si = *reinterpret_cast<const float2*>(tab + a.rot / 2 + c);
+          cs[c] = co.x; cs[c + 1] = co.y; sn[c] = si.x; sn[c + 1] = si.y;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      const int h = h0 + i * lanes;
+      if (h >= heads) continue;
+      const bool is_v = h >= a.Hq + a.kv.Hkv;
+      T* out = h < a.Hq ? (T*)a.q_out + row * a.q_out_stride + (long long)h * hd
+                        : (T*)(is_v ? a.kv.v : a.kv.k) + at + (long long)(h - a.Hq - (is_v ? a.kv.Hkv : 0)) * a.kv.head_stride;
+      if (!turns || is_v) {
+        *reinterpret_cast<uint4*>(out + c0) = x[i][0];
+        if (HALVES && two) *reinterpret_cast<uint4*>(out + c1) = x[i][HALVES ? 1 : 0];
+        continue;
+      }
       float xa[N];
       Vec<T>::get(x[i][0], xa);
-      if (HALVES) {
+      if constexpr (HALVES) {
         float xb[N], ya[N], yb[N];
         Vec<T>::get(x[i][1], xb);
 #pragma unroll
-        for (int c = 0; c < N; c += 4) {
-          const float4 co = *reinterpret_cast<const float4*>(tab + c), si = *reinterpret_cast<const float4*>(tab + a.rot / 2 + c);
-          const float cs[4] = {co.x, co.y, co.z, co.w}, sn[4] = {si.x, si.y, si.z, si.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            ya[c + e] = xa[c + e] * cs[e] - xb[c + e] * sn[e];
-            yb[c + e] = xb[c + e] * cs[e] + xa[c + e] * sn[e];
-          }
-        }
-        *reinterpret_cast<uint4*>(out) = Vec<T>::put(ya);
-        *reinterpret_cast<uint4*>(out + t.second) = Vec<T>::put(yb);
+        for (int c = 0; c < N; ++c) { ya[c] = xa[c] * cs[c] - xb[c] * sn[c]; yb[c] = xb[c] * cs[c] + xa[c] * sn[c]; }
+        *reinterpret_cast<uint4*>(out + c0) = Vec<T>::put(ya);
+        *reinterpret_cast<uint4*>(out + c1) = Vec<T>::put(yb);
       } else {
         float y[N];
 #pragma unroll
-        for (int c = 0; c < N / 2; c += 2) {
-          const float2 co = *reinterpret_cast<const float2*>(tab + c), si = *reinterpret_cast<const float2*>(tab + a.rot / 2 + c);
-          y[2 * c] = xa[2 * c] * co.x - xa[2 * c + 1] * si.x;
-          y[2 * c + 1] = xa[2 * c + 1] * co.x + xa[2 * c] * si.x;
-          y[2 * c + 2] = xa[2 * c + 2] * co.y - xa[2 * c + 3] * si.y;
-          y[2 * c + 3] = xa[2 * c + 3] * co.y + xa[2 * c + 2] * si.y;
+        for (int c = 0; c < N; c += 2) {
+          y[c] = xa[c] * cs[c / 2] - xa[c + 1] * sn[c / 2];
+          y[c + 1] = xa[c + 1] * cs[c / 2] + xa[c] * sn[c / 2];
         }
-        *reinterpret_cast<uint4*>(out) = Vec<T>::put(y);
+        *reinterpret_cast<uint4*>(out + c0) = Vec<T>::put(y);
       }
     }
   }
@@ -234,14 +222,15 @@ __global__ void rope_table_kernel(const __grid_constant__ RopeFrequencies f, flo
 template <typename T, bool HALVES>
 void launch_vec(const AppendArgs& a, cudaStream_t st) {
   constexpr int N = Vec<T>::N;
-  const int per_turned = (HALVES ? a.rot / 2 / N : a.rot / N) + (a.kv.hd - a.rot) / N, per_copied = a.kv.hd / N;
-  const int units = (a.Hq + a.kv.Hkv) * per_turned + a.kv.Hkv * per_copied;
-  const int threads = units >= 1024 ? 1024 : (units + 31) / 32 * 32;
-  // rows per block: as many as keep the grid above two waves of blocks
-  if (a.kv.rows > 4 * 148 * 4)
-    launch_pdl(kv_append_kernel<T, HALVES, 4>, dim3((a.kv.rows + 3) / 4), dim3(threads), 0, st, a, units, per_turned, per_copied);
-  else
-    launch_pdl(kv_append_kernel<T, HALVES, 1>, dim3(a.kv.rows), dim3(threads), 0, st, a, units, per_turned, per_copied);
+  const int turned = HALVES ? a.rot / 2 / N : a.rot / N, units = turned + (a.kv.hd - a.rot) / N, heads = a.Hq + 2 * a.kv.Hkv;
+  // heads side by side: as few as keep all of a row's loads under way at once, and few rows' threads together a block of 128 or more
+  int lanes = (heads + kHeads - 1) / kHeads;
+  if (lanes * units > 1024) lanes = 1024 / units;
+  int rows = 1;
+  if (a.kv.rows > 8 * 148)
+    while (rows < 16 && 2 * rows * lanes * units <= 256) rows *= 2;
+  const int threads = (rows * lanes * units + 31) / 32 * 32;
+  launch_pdl(kv_append_kernel<T, HALVES>, dim3((a.kv.rows + rows - 1) / rows), dim3(threads), 0, st, a, units, turned, lanes, rows);
 }
 
 template <typename T>

@@ -19,7 +19,7 @@ void launch_paged_attn_tc(const PagedAttnArgs& a, int rows, cudaStream_t st);
 
 namespace {
 
-enum { kSimt = 0, kTc16 = 1, kTc64 = 2, kUmma = 3 };
+enum { kSimt = 0, kTc16 = 1, kTc64 = 2, kUmma = 3, kToken = 4 };
 constexpr int kMaxSplits = 64;
 constexpr int kRowsS = 16, kPosS = 32, kWarpsS = 4, kRowsWarp = kRowsS / kWarpsS;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -172,18 +172,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArg
     const int i = lane + 32 * h;
     w[h] = i < a.splits ? a.part_lse[i * n + rh] : -INFINITY;
   }
-  // rows that no sequence has are left alone (a split wrote nothing for them)
-  int lo = 0, hi = a.kv.batch + 1;
-  while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-    const int c = __popc(__ballot_sync(0xffffffffu, at < hi && a.kv.row_start[at] <= row));
-    if (c == 0) break;
-    hi = min(hi, lo + c * step);
-    lo += (c - 1) * step + 1;
-  }
-  if (lo < 1 || lo > a.kv.batch) return;
-  const PagedSeq s = paged_seq(a.kv, lo - 1, false);
-  if (row < s.row0 || row >= s.row0 + s.n) return;
   m = warp_max(fmaxf(w[0], w[1]));
   const bool none = m == -INFINITY && !__any_sync(0xffffffffu, w[0] != w[0] || w[1] != w[1]);
   unsigned seen[2];
@@ -217,6 +205,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArg
   if (HD >= 32 || lane < 16)
 #pragma unroll
     for (int d = 0; d < DL; ++d) sums[warp][col + d] = o[d];
+  // rows that no sequence has are left alone (no split wrote anything for them; looked up while the parts are on their way)
+  int lo = 0, hi = a.kv.batch + 1;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const int c = __popc(__ballot_sync(0xffffffffu, at < hi && a.kv.row_start[at] <= row));
+    if (c == 0) break;
+    hi = min(hi, lo + c * step);
+    lo += (c - 1) * step + 1;
+  }
+  if (lo < 1 || lo > a.kv.batch) return;
+  const PagedSeq s = paged_seq(a.kv, lo - 1, false);
+  if (row < s.row0 || row >= s.row0 + s.n) return;
   __syncthreads();
   const float inv = none ? 0.f : 1.f / sum;
   T* out = (T*)a.out + row * a.out_stride + (long long)head * HD;
@@ -262,6 +262,7 @@ PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
     tile_rows = rows <= 16 ? 16 : 64;
     per_sm = rows <= 16 ? 6 : 2;
     least = rows <= 16 ? 8 : 4;
+    if (rows <= 8) p.kernel = kToken;
     if (rows > 64 && a.kv.page_size % 8 == 0) { p.kernel = kUmma; tile_rows = 256; per_sm = 1; least = 8; }
   }
   const long long tiles = (a.kv.max_kv + kAttnTile - 1) / kAttnTile;
@@ -286,8 +287,9 @@ void launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan
   if (plan.splits > 1) a.part_lse = a.part_o + (long long)plan.splits * a.kv.rows * a.Hq * a.kv.hd;
   LaunchScope ls(kcAttention, st, plan.splits > 1 ? 2 : 1);
   if (plan.kernel == kUmma && launch_paged_attn_umma(a, st)) {}
+  else if (plan.kernel == kToken) launch_paged_attn_tc(a, 8, st);
   else if (plan.kernel == kTc16) launch_paged_attn_tc(a, 16, st);
-  else if (plan.kernel >= kTc64) launch_paged_attn_tc(a, 64, st);
+  else if (plan.kernel == kTc64 || plan.kernel == kUmma) launch_paged_attn_tc(a, 64, st);
   else if (bf16) launch_simt<__nv_bfloat16>(a, st);
   else launch_simt<float>(a, st);
   if (plan.splits > 1) {
