@@ -75,12 +75,20 @@ __device__ __forceinline__ void produce(const CUtensorMap& tmK, const CUtensorMa
   auto full_bar = [&](int kv, int s) { return bar_base + 8u * (2 * s + kv); };
   auto empty_bar = [&](int kv, int s) { return bar_base + 8u * (2 * (S + s) + kv); };
   // Two rings, whichever has a free slot is served: a K slot is free again after the scores, its V slot only at the end of the tile (one ring of
-  // pairs: 64 tokens on up to 4,000 positions 142 us).
+  // pairs: 64 tokens on up to 4,000 positions 142 us).  The boxes of all tiles are numbered through; a lane looks up the page of one box in 32, for each ring,
+  // 32 boxes ahead (looked up tile by tile, a page's way from memory was in every tile's: 64 tokens, heads of 64, 4,000 positions 120 us).
   const uint32_t leader = elect_one();
   const int nb = PAGES ? kPos / box_rows : 0;
-  int t[2] = {0, 0}, page[2] = {0, 0};             // the next tile of each ring, and (lane i) the page of its box i
-  auto look_up = [&](int tile) { return tile < NT && lane < nb ? page_of(a.kv, b, (t_begin + tile) * kPos + lane * box_rows, box_rows, u_lo, u_hi) : 0; };
-  if constexpr (PAGES) page[0] = page[1] = look_up(0);
+  int t[2] = {0, 0}, y[2], page[2] = {0, 0}, next[2] = {0, 0};      // the next tile of each ring, its place in its page; pages of this and the next 32 boxes
+  auto look_up = [&](int box) {
+    box += lane;
+    return box < NT * nb ? page_of(a.kv, b, t_begin * kPos + box * box_rows, box_rows, u_lo, u_hi) : 0;
+  };
+  if constexpr (PAGES) {
+    y[0] = y[1] = t_begin * kPos % a.kv.page_size;
+    page[0] = page[1] = look_up(0);
+    next[0] = next[1] = look_up(32);
+  }
   bool ok = true;
   long long since = clock64();
   while (t[0] < NT || t[1] < NT) {
@@ -92,15 +100,15 @@ __device__ __forceinline__ void produce(const CUtensorMap& tmK, const CUtensorMa
       const uint32_t dst = base + s * 2 * kTileBytes + kv * kTileBytes, bar = full_bar(kv, s);
       if constexpr (PAGES) {
         mbar_expect_tx_if(bar, kTileBytes, leader);
-        int y = (t_begin + t[kv]) * kPos % a.kv.page_size;
+        const int first = t[kv] * nb;
+        if (t[kv] > 0 && (first & 31) == 0) { page[kv] = next[kv]; next[kv] = look_up(first + 32); }      // (nb divides 32)
         for (int i = 0; i < nb; ++i) {
-          const int pg = __shfl_sync(0xffffffffu, page[kv], i);
+          const int pg = __shfl_sync(0xffffffffu, page[kv], (first + i) & 31);
 #pragma unroll
-          for (int h = 0; h < NH; ++h) tma_load_4d_if(dst + h * (kPos * 128) + i * box_rows * 128, kv ? &tmV : &tmK, h * 64, y, kvh, pg, bar, leader);
-          y += box_rows;
-          if (y >= a.kv.page_size) y -= a.kv.page_size;
+          for (int h = 0; h < NH; ++h) tma_load_4d_if(dst + h * (kPos * 128) + i * box_rows * 128, kv ? &tmV : &tmK, h * 64, y[kv], kvh, pg, bar, leader);
+          y[kv] += box_rows;
+          if (y[kv] >= a.kv.page_size) y[kv] -= a.kv.page_size;
         }
-        page[kv] = look_up(t[kv] + 1);
       } else {
         for (int i = 0; i < kPos; i += 32) {       // a lane looks a position up, the warp copies the 32 of them
           const int p = (t_begin + t[kv]) * kPos + i + lane;
