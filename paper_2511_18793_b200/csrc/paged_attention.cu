@@ -7,7 +7,8 @@
 // row tile and not once per head.  A context is split over CTAs where sequences, heads and row tiles leave SMs idle; the parts
 // (their own maximum and sum: o and log2 of the sum) are joined by attn_join_kernel in the order of the splits.
 #include <math.h>
-#include <stdlib.h>
+
+#include <algorithm>
 
 #include "operators.cuh"
 
@@ -253,31 +254,45 @@ void launch_join(const PagedAttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+// Tiles of kAttnTile positions that a CTA of `rows` query rows goes through at most: all of a sequence's, or what a window lets them see.
+static long long tiles_seen(const PagedAttnArgs& a, int rows) {
+  long long span = a.kv.max_kv;
+  if (a.window > 0) span = std::min(span, (long long)a.window + rows / a.G + 1 + kAttnTile);
+  return (span + kAttnTile - 1) / kAttnTile;
+}
+
 PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
   PagedAttnPlan p{kSimt, 1, 0, 0};
-  const long long rows = (long long)a.kv.max_new * a.G;
-  int tile_rows = kRowsS, per_sm = 4, least = 2;
-  if (bf16 && a.kv.hd >= 64) {
-    p.kernel = rows <= 16 ? kTc16 : kTc64;
-    tile_rows = rows <= 16 ? 16 : 64;
-    per_sm = rows <= 16 ? 6 : 2;
-    least = rows <= 16 ? 8 : 4;
-    if (rows <= 8) p.kernel = kToken;
-    if (rows > 64 && a.kv.page_size % 8 == 0) { p.kernel = kUmma; tile_rows = 256; per_sm = 1; least = 8; }
+  const long long rows = (long long)a.kv.max_new * a.G, tiles = (a.kv.max_kv + kAttnTile - 1) / kAttnTile;
+  const long long pairs = (long long)a.kv.Hkv * a.kv.batch;
+  long long s = 1;
+  if (bf16 && a.kv.hd >= 64 && rows > 64 && a.kv.page_size % 8 == 0) {
+    // Many rows: one CTA per SM.  A context is split where that gives idle SMs something to do, but not to even out the last wave of many: 512 CTAs (3.5
+    // waves) as they are 1,094 us, in halves 1,158 (the parts' way through memory, and less idle silicon to leave the others its power).
+    p.kernel = kUmma;
+    const long long units = pairs * ((rows + 255) / 256);
+    s = std::min(sm_count() / std::max(units, 1ll), (tiles_seen(a, 256) + 3) / 4);
+  } else {
+    int tile_rows = kRowsS, per_sm = 4, least = 2;
+    if (bf16 && a.kv.hd >= 64) {
+      p.kernel = rows <= 8 ? kToken : rows <= 16 ? kTc16 : kTc64;
+      tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 64;
+      per_sm = rows <= 16 ? 9 : 2;
+      least = rows <= 16 ? 8 : 4;
+    }
+    const long long ctas = pairs * ((rows + tile_rows - 1) / tile_rows);
+    s = std::min((per_sm * (long long)sm_count() + ctas - 1) / std::max(ctas, 1ll), tiles_seen(a, tile_rows) / least);
   }
-  const long long tiles = (a.kv.max_kv + kAttnTile - 1) / kAttnTile;
-  const long long ctas = (long long)a.kv.Hkv * a.kv.batch * ((rows + tile_rows - 1) / tile_rows);
-  static const int f1 = getenv("X_PER") ? atoi(getenv("X_PER")) : 0, f2 = getenv("X_LEAST") ? atoi(getenv("X_LEAST")) : 0;
-  if (f1) per_sm = f1;
-  if (f2) least = f2;
-  long long s = (per_sm * (long long)sm_count() + ctas - 1) / ctas;
-  if (s > tiles / least) s = tiles / least;
-  if (s > kMaxSplits) s = kMaxSplits;
+  s = std::min(s, (long long)kMaxSplits);
   if (s > 1) {
-    p.split_tiles = (int)((tiles + s - 1) / s + 1) / 2 * 2;
+    // (a window moves along the sequence, so all its positions are dealt out, in shares of what a row tile sees of them)
+    const long long share = (tiles_seen(a, p.kernel == kUmma ? 256 : 16) + s - 1) / s;
+    p.split_tiles = (int)((share + 1) / 2 * 2);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
+    if (p.splits > kMaxSplits) { p.split_tiles = (int)((tiles + kMaxSplits - 1) / kMaxSplits + 1) / 2 * 2; p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles); }
   }
   if (p.splits > 1) p.bytes = (size_t)p.splits * a.kv.rows * a.Hq * (a.kv.hd + 1) * sizeof(float);
+  else { p.splits = 1; p.split_tiles = 0; }
   return p;
 }
 

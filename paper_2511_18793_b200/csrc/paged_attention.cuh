@@ -65,6 +65,16 @@ __device__ __forceinline__ int page_of(const PagedView& kv, int b, int t, int n,
   return page;
 }
 
+// Eight bf16 values: is one of them infinite or not a number; and with zeros in the place of those.  (An exponent of ones is the only one that a further
+// step carries into the sign's bit.)
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ bool any_odd(const uint4& x) { return (odd_bits(x.x) | odd_bits(x.y) | odd_bits(x.z) | odd_bits(x.w)) != 0u; }
+__device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+  const uint32_t o = odd_bits(w);
+  return w & ~((o >> 15) * 0xffffu);
+}
+__device__ __forceinline__ uint4 without_odd(const uint4& x) { return make_uint4(without_odd(x.x), without_odd(x.y), without_odd(x.z), without_odd(x.w)); }
+
 // tanh to about 2e-7 absolute (relative below 1/4, by its series: a cap far above the scores must not cost them digits).
 __device__ __forceinline__ float tanh_fast(float y) {
   const float z = y * y;

@@ -53,15 +53,7 @@ __device__ __forceinline__ void clear_values(uint8_t* v, int p0, int u_lo, int u
     if (p >= c_lo && p < c_hi) continue;
     uint4* at = reinterpret_cast<uint4*>(v + kv_off(i / CH, i % CH));
     if (p < u_lo || p >= u_hi) { *at = make_uint4(0u, 0u, 0u, 0u); continue; }
-    uint4 x = *at;
-    uint32_t* w = reinterpret_cast<uint32_t*>(&x);
-    bool odd = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; odd = true; }
-      if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; odd = true; }
-    }
-    if (odd) { *at = x; *odd_flag = 1; }
+    if (any_odd(*at)) { *at = without_odd(*at); *odd_flag = 1; }
   }
   __syncwarp();
 }

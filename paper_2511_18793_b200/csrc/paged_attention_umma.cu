@@ -25,6 +25,7 @@ using namespace paged_detail;
 
 constexpr int kPosP = 128;         // positions per tile
 constexpr int kThreadsP = 384;     // warps 0 to 3: copies, products, two idle; 4 to 7: rows A; 8 to 11: rows B
+constexpr int kRegsRest = 88, kRegsSoftmax = 208;       // registers a thread; together what 384 threads of 168 have
 constexpr float kRaise = 8.f;
 
 template <int HD> struct UCfg {
@@ -99,6 +100,7 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
 
 // tanh(y) / y as a polynomial in y^2, |y| <= 0.6: fitted to tanh for the least relative error, 8e-8.
 constexpr float kTanhRange = 0.6f;
+constexpr float kTanhNear = 0.2f, kTanhShort[3] = {0.99999988f, -0.3332859f, 0.13015407f};      // and for |y| <= 0.2: 1.1e-7
 constexpr float kTanh[5] = {0.99999994f, -0.33332309f, 0.13310173f, -0.052101482f, 0.015475428f};
 
 // FORM, a sum of: scores capped; scores biased by their distance (or a scale that is not positive).  0: neither.
@@ -181,7 +183,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   const uint32_t tmem_base = *tmem_slot;
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
     if (warp == 0) {
       // ------------------------------------------------------------------ copies: K_0, V_0, K_1, V_1, ... through one ring
       const uint32_t leader = elect_one();
@@ -265,7 +267,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
       if (!ok && leader) *abort_flag = 1;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // ------------------------------------------------------------------ softmax, one thread per row
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem_base + lane_addr + 128u * x, t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
@@ -301,8 +303,16 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 #pragma unroll
             for (int q = 0; q < 4; ++q) mb[q] = fmaxf(mb[q], fabsf(sv[c + q]));
           // (positions that nobody sees may be beyond; a NaN among them is not noticed here and stays one below)
-          if (__all_sync(0xffffffffu, fmaxf(fmaxf(mb[0], mb[1]), fmaxf(mb[2], mb[3])) * fabsf(inv_cap) <= kTanhRange)) {
-            const float i2 = inv_cap * inv_cap, lead = cap2 * inv_cap;
+          const float top = fmaxf(fmaxf(mb[0], mb[1]), fmaxf(mb[2], mb[3])) * fabsf(inv_cap), i2 = inv_cap * inv_cap, lead = cap2 * inv_cap;
+          if (__all_sync(0xffffffffu, top <= kTanhNear)) {
+            const float c0 = kTanhShort[0] * lead, c1 = kTanhShort[1] * lead * i2, c2 = kTanhShort[2] * lead * i2 * i2;
+            const f32x2 k0 = pack2(c0, c0), k1 = pack2(c1, c1), k2 = pack2(c2, c2);
+#pragma unroll
+            for (int c = 0; c < kPosP; c += 2) {
+              const f32x2 v = pack2(sv[c], sv[c + 1]), z = mul2(v, v);
+              unpack2(mul2(v, fma2(z, fma2(z, k2, k1), k0)), sv[c], sv[c + 1]);
+            }
+          } else if (__all_sync(0xffffffffu, top <= kTanhRange)) {
             const f32x2 k0 = pack2(kTanh[0] * lead, kTanh[0] * lead), i22 = pack2(i2, i2);
             const f32x2 k1 = pack2(kTanh[1] * lead, kTanh[1] * lead), k2 = pack2(kTanh[2] * lead, kTanh[2] * lead);
             const f32x2 k3 = pack2(kTanh[3] * lead, kTanh[3] * lead), k4 = pack2(kTanh[4] * lead, kTanh[4] * lead);
@@ -332,10 +342,17 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(-slope, fabsf(rel - (float)c), sv[c]);
           }
         }
-        if (edge) {
+        if (j < j_lo) {                              // (a tile is seldom on both edges)
+          const int from = vis.lo - p0;
 #pragma unroll
           for (int c = 0; c < kPosP; ++c)
-            if (p0 + c < vis.lo || p0 + c >= vis.hi) sv[c] = -INFINITY;
+            if (c < from) sv[c] = -INFINITY;
+        }
+        if (j >= j_hi) {
+          const int to = vis.hi - p0;
+#pragma unroll
+          for (int c = 0; c < kPosP; ++c)
+            if (c >= to) sv[c] = -INFINITY;
         }
         float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -367,21 +384,14 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
           if (!ok) break;
           uint8_t* vg = gen_base + (ring - base) + ((2 * j + 1) % SR) * C::kTileBytes + row * 128;
           const int p = p0 + row;
-          if (p < u_lo || p >= u_hi) {
-#pragma unroll
-            for (int c = 0; c < HD / 8; ++c) *reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-          } else if (p < c_lo || p >= c_hi) {
-            for (int c = 0; c < HD / 8; ++c) {
+          if (p < c_lo || p >= c_hi) {               // (neighbouring threads take a row's pieces in different orders: 16 bytes of each of 8 rows are 128 of the banks)
+            const bool unseen = p < u_lo || p >= u_hi;
+#pragma unroll 4
+            for (int i = 0; i < HD / 8; ++i) {
+              const int c = i ^ (row & 7);
               uint4* at = reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4));
-              uint4 v = *at;
-              uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-              bool odd = false;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; odd = true; }
-                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; odd = true; }
-              }
-              if (odd) { *at = v; *odd_flag = 1; }
+              if (unseen) *at = make_uint4(0u, 0u, 0u, 0u);
+              else if (any_odd(*at)) { *at = without_odd(*at); *odd_flag = 1; }
             }
           }
           fence_async();
@@ -488,11 +498,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   if (threadIdx.x == 0 && *abort_flag) atomicOr(a.kv.status, kStInternal);
 }
 
-// The softmax warpgroups take 224 registers a thread and leave 56 to the other: the launch has to have 168 for all (else they would wait).
+// The softmax warpgroups take more registers a thread and leave the other fewer: the launch has to have them all (else they would wait).
 template <int HD, int FORM>
 bool registers_add_up() {
   cudaFuncAttributes at{};
-  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM>) == cudaSuccess && at.numRegs * kThreadsP >= 56 * 128 + 224 * 256;
+  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM>) == cudaSuccess && at.numRegs * kThreadsP >= kRegsRest * 128 + kRegsSoftmax * 256;
 }
 
 template <int HD, int FORM>
