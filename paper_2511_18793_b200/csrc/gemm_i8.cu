@@ -113,11 +113,13 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_kernel(const __grid_constant
     int t_local = 0;
     bool ok = true;
     for (int tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x, ++t_local) {
-      const int b = t_local & 1;
+      const int b = t_local & 1, m0 = (tile % tiles_m) * 128, n0 = (tile / tiles_m) * BN;
+      TileScales<BN> ts;
+      ts.get(a, q, half, lane, m0, n0);
       ok = warp_wait_uniform(acc_full(b), (t_local >> 1) & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
-      drain<BN, OUT>(a, tmem_base + (uint32_t)(b * BN), q, half, lane, stg, (tile % tiles_m) * 128, (tile / tiles_m) * BN, wide);
+      drain<BN, OUT>(a, tmem_base + (uint32_t)(b * BN), q, half, lane, stg, m0, n0, wide, ts);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(acc_empty(b));
@@ -243,11 +245,13 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_pair_kernel(const __grid_con
     bool ok = true;
     for (int tile = pair; tile < n_tiles && ok; tile += n_pairs, ++t_local) {
       const TileMN tt = tile_of(tile, tiles_m, tiles_n, band);
-      const int b = t_local & 1;
+      const int b = t_local & 1, m0 = tt.m * 256 + (int)rank * 128, n0 = tt.n * kPairN;
+      TileScales<kPairN> ts;
+      ts.get(a, q, half, lane, m0, n0);
       ok = warp_wait_uniform(acc_full(b), (t_local >> 1) & 1, abort_flag);
       if (!ok) break;
       tc_fence_after();
-      drain<kPairN, OUT>(a, tmem_base + (uint32_t)(b * kPairN), q, half, lane, stg, tt.m * 256 + (int)rank * 128, tt.n * kPairN, wide);
+      drain<kPairN, OUT>(a, tmem_base + (uint32_t)(b * kPairN), q, half, lane, stg, m0, n0, wide, ts);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(acc_empty(b) & kLeaderMask) : "memory");

@@ -23,7 +23,7 @@ template <int MT> struct SkCfg {
   static_assert(MT * 128 * 4 <= kStages * kStage, "the sums do not fit in the ring");
   static_assert(2 * (kSmem + 1024) <= 228 * 1024, "two CTAs per SM");
 };
-constexpr int kSkEpiWarps = 4, kSkThreads = 64 + 32 * kSkEpiWarps;
+constexpr int kSkEpiWarps = 8, kSkThreads = 64 + 32 * kSkEpiWarps;
 
 __device__ __forceinline__ int4 ld_peer(uint32_t local, uint32_t rank) {
   uint32_t ra;
@@ -33,7 +33,7 @@ __device__ __forceinline__ int4 ld_peer(uint32_t local, uint32_t rank) {
   return v;
 }
 
-// grid = tiles x splits, clusters of `splits` CTAs.  Warp 0: TMA; warp 1: TMEM and MMA; warps 2 to 5: sums and stores.
+// grid = tiles x splits, clusters of `splits` CTAs.  Warp 0: TMA; warp 1: TMEM and MMA; warps 2 to 9: sums and stores.
 template <int MT, int OUT>
 __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, GemmI8Args a,
                                                                       int splits) {
@@ -60,6 +60,11 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
     tma_prefetch_map(&tmW);
     tma_prefetch_map(&tmX);
   }
+  // The first of this CTA's weights into the L2 while the launch before is still running (a copy there is no older than memory: what that launch writes
+  // is in it).
+  if (threadIdx.x == 64)
+    for (int k = 0; k < min(STAGES, k_count); ++k)
+      asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(&tmW), "r"((k_begin + k) * kStepK), "r"(n0) : "memory");
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(C::kTmemCols));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -70,7 +75,8 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
   const uint32_t tmem_base = *tmem_slot;
   pdl_wait();
   pdl_launch();
-  float sw[4], bias[4];
+  // A row of the sums goes to one of the cluster's epilogue warps: this one's i-th is split + splits * (warp - 2 + 8 i); lane i has its scale.
+  float sw[4], bias[4], sa_mine = 0.f;
   if (warp == 0) {
     const uint32_t leader = elect_one();
     int s = 0, k = 0;
@@ -106,6 +112,8 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
     else if (leader) *abort_flag = 1;
   } else {
     cols4(a, n0 + 4 * lane, sw, bias);
+    const int r = split + splits * (warp - 2 + kSkEpiWarps * lane);
+    if (r < a.M) sa_mine = a.a_scale[r];
     const bool ok = warp_wait_uniform(acc_full, 0, abort_flag);
     tc_fence_after();
     if (ok) {
@@ -113,11 +121,11 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
       const int q = warp & 3;
       int* img = reinterpret_cast<int*>(gen_base) + q * 32 + lane;
 #pragma unroll 1
-      for (int r0 = 0; r0 < min(MT, a.M); r0 += 32) {
-        int v[32];
-        tmem_ld32_int(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)r0, v);
+      for (int r0 = (warp - 2) / 4 * 16; r0 < min(MT, a.M); r0 += 32) {      // (the two warps of a lane quarter take 16 rows each in turn)
+        int v[16];
+        tmem_ld16_int(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)r0, v);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) img[(r0 + j) * 128] = v[j];
+        for (int j = 0; j < 16; ++j) img[(r0 + j) * 128] = v[j];
       }
     } else if (lane == 0) {
       *abort_flag = 1;
@@ -129,7 +137,10 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
   if (warp >= 2 && !*abort_flag) {
     const bool wide = wide_rows<OUT>(a) && n0 + 4 * lane + 3 < a.N;
     const uint32_t at = base + lane * 16;
-    for (int r = split + splits * (warp - 2); r < a.M; r += splits * kSkEpiWarps) {
+    int i = 0;
+#pragma unroll 2
+    for (int r = split + splits * (warp - 2); r < a.M; r += splits * kSkEpiWarps, ++i) {
+      const float sa = __shfl_sync(0xffffffffu, sa_mine, i);
       int4 part[8];
 #pragma unroll
       for (int p = 0; p < 8; ++p)
@@ -138,7 +149,7 @@ __global__ void __launch_bounds__(kSkThreads, 2) gemm_i8_skinny_kernel(const __g
 #pragma unroll
       for (int p = 1; p < 8; ++p)
         if (p < splits) { acc[0] += part[p].x; acc[1] += part[p].y; acc[2] += part[p].z; acc[3] += part[p].w; }
-      if (n0 + 4 * lane < a.N) store4<OUT>(a, r, n0 + 4 * lane, acc, a.a_scale[r], sw, bias, wide);
+      if (n0 + 4 * lane < a.N) store4<OUT>(a, r, n0 + 4 * lane, acc, sa, sw, bias, wide);
     }
   }
   if (splits > 1) cluster_sync_all();                // no CTA leaves while a peer may still read its sums
