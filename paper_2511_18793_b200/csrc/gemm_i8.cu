@@ -321,7 +321,11 @@ void launch_gemm_i8(const GemmI8Args& a, bool bf16, cudaStream_t st) {
   const bool bf16_out = bf16 && a.epilogue == kEpiStoreAct;
   const bool tc = a.K % 16 == 0 && ((uintptr_t)a.A & 15) == 0 && ((uintptr_t)a.W & 15) == 0 && tma_encode_fn();
   if (tc) {
-    if (a.M <= 128 && launch_gemm_i8_skinny(a, bf16_out, st)) return;
+    // Few rows stream the weights with W as the 128-row operand; beyond 32 of them only where that splits the K range three ways or more, which is what the
+    // general kernel's wider tiles then lose by.  us, streaming / general, 48 rows: 6144 x 4096 11.4 / 10.8, 22016 x 4096 25.6 / 24.5, 2048 x 8192 10.3 / 13.3,
+    // 4096 x 11008 16.4 / 19.4; 100 rows: 13.6 / 11.0, 29.4 / 24.9, 12.2 / 13.5, 18.1 / 19.7; 20 rows: 10.4 / 15.6, 23.3 / 26.9, 8.9 / 13.2, 14.8 / 19.1.
+    const bool streams = a.M <= 32 || (a.M <= 128 && sm_count() / ((a.N + 127) / 128) >= 3);
+    if (streams && launch_gemm_i8_skinny(a, bf16_out, st)) return;
     if (bf16_out ? launch_tiles<kBf16>(a, st) : a.epilogue == kEpiAddF32 ? launch_tiles<kF32Add>(a, st) : launch_tiles<kF32>(a, st)) return;
   }
   launch_gemm_i8_simt(a, bf16, st);
