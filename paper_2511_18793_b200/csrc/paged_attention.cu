@@ -154,19 +154,21 @@ __global__ void __launch_bounds__(32 * kWarpsS) paged_attn_simt_kernel(PagedAttn
   }
 }
 
-// A block per (row, head): the parts weighted by their sums.  Warp w adds the parts w, w + 4, ... in their order, all of whose loads are under way
-// together (a warp per row and head that skipped empty parts by a branch: one load at a time, 57 parts 20 us), the four sums are added in order.
+// JW warps per (row, head): the parts weighted by their sums.  Warp w adds the parts w, w + JW, ... in their order, all of whose loads are under way
+// together (a warp that skipped empty parts by a branch: one load at a time, 57 parts 20 us), the warps' sums are added in order.  Four warps where there
+// are many parts, one, and four rows and heads per block, where there are few (8,352 of them in 3 parts: 12 us with a block each).
 constexpr int kJoinWarps = 4;
-template <typename T, int HD>
+template <typename T, int HD, int JW>
 __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArgs a) {
   __shared__ float sums[kJoinWarps][HD];
   pdl_wait();
   pdl_launch();
-  const long long rh = blockIdx.x;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) % JW, group = (threadIdx.x >> 5) / JW;
+  const long long rh = (long long)blockIdx.x * (kJoinWarps / JW) + group, all = (long long)a.kv.rows * a.Hq;
+  if (JW < kJoinWarps && rh >= all) return;         // (a whole warp; nothing is waited for below)
   const int row = (int)(rh / a.Hq), head = (int)(rh - (long long)row * a.Hq);
   // a lane looks after two parts' weights (kMaxSplits of them at most)
-  const long long n = (long long)a.kv.rows * a.Hq;
+  const long long n = all;
   float w[2], m = -INFINITY;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -189,9 +191,9 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArg
 #pragma unroll
   for (int d = 0; d < DL; ++d) o[d] = 0.f;
   const int col = HD >= 32 ? lane * DL : lane & 15;
-#pragma unroll
-  for (int j = 0; j < kMaxSplits / kJoinWarps; ++j) {
-    const int i = warp + kJoinWarps * j;
+#pragma unroll(JW == 1 ? 8 : kMaxSplits / JW)
+  for (int j = 0; j < kMaxSplits / JW; ++j) {
+    const int i = warp + JW * j;
     if (i >= a.splits) break;
     const float wi = __shfl_sync(0xffffffffu, i < 32 ? w[0] : w[1], i & 31);
     const bool on = (i < 32 ? seen[0] : seen[1]) >> (i & 31) & 1u;          // (else nothing was written for it)
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArg
   }
   if (HD >= 32 || lane < 16)
 #pragma unroll
-    for (int d = 0; d < DL; ++d) sums[warp][col + d] = o[d];
+    for (int d = 0; d < DL; ++d) sums[group * JW + warp][col + d] = o[d];
   // rows that no sequence has are left alone (no split wrote anything for them; looked up while the parts are on their way)
   int lo = 0, hi = a.kv.batch + 1;
   while (lo < hi) {
@@ -218,16 +220,17 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(PagedAttnArg
   if (lo < 1 || lo > a.kv.batch) return;
   const PagedSeq s = paged_seq(a.kv, lo - 1, false);
   if (row < s.row0 || row >= s.row0 + s.n) return;
-  __syncthreads();
+  if (JW > 1) __syncthreads();                       // (all warps of a row and head return above, or none)
+  else __syncwarp();
   const float inv = none ? 0.f : 1.f / sum;
   T* out = (T*)a.out + row * a.out_stride + (long long)head * HD;
-  for (int d = threadIdx.x; d < HD; d += 32 * kJoinWarps) {
+  for (int d = warp * 32 + lane; d < HD; d += 32 * JW) {
     float x = 0.f;
 #pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) x += sums[i][d];
+    for (int i = 0; i < JW; ++i) x += sums[group * JW + i][d];
     out[d] = from_f32<T>(x * inv);
   }
-  if (a.lse && threadIdx.x == 0) a.lse[rh] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+  if (a.lse && warp == 0 && lane == 0) a.lse[rh] = none ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
 }
 
 template <typename T>
@@ -241,14 +244,15 @@ void launch_simt(const PagedAttnArgs& a, cudaStream_t st) {
     default: launch_pdl(paged_attn_simt_kernel<T, 128>, grid, dim3(32 * kWarpsS), 0, st, a, row_tiles); break;
   }
 }
-template <typename T>
+template <typename T, int JW>
 void launch_join(const PagedAttnArgs& a, cudaStream_t st) {
-  const dim3 grid((unsigned)((long long)a.kv.rows * a.Hq)), block(32 * kJoinWarps);
+  constexpr int kRows = kJoinWarps / JW;
+  const dim3 grid((unsigned)(((long long)a.kv.rows * a.Hq + kRows - 1) / kRows)), block(32 * kJoinWarps);
   switch (a.kv.hd) {
-    case 16: launch_pdl(attn_join_kernel<T, 16>, grid, block, 0, st, a); break;
-    case 32: launch_pdl(attn_join_kernel<T, 32>, grid, block, 0, st, a); break;
-    case 64: launch_pdl(attn_join_kernel<T, 64>, grid, block, 0, st, a); break;
-    default: launch_pdl(attn_join_kernel<T, 128>, grid, block, 0, st, a); break;
+    case 16: launch_pdl(attn_join_kernel<T, 16, JW>, grid, block, 0, st, a); break;
+    case 32: launch_pdl(attn_join_kernel<T, 32, JW>, grid, block, 0, st, a); break;
+    case 64: launch_pdl(attn_join_kernel<T, 64, JW>, grid, block, 0, st, a); break;
+    default: launch_pdl(attn_join_kernel<T, 128, JW>, grid, block, 0, st, a); break;
   }
 }
 
@@ -308,8 +312,9 @@ void launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan
   else if (bf16) launch_simt<__nv_bfloat16>(a, st);
   else launch_simt<float>(a, st);
   if (plan.splits > 1) {
-    if (bf16) launch_join<__nv_bfloat16>(a, st);
-    else launch_join<float>(a, st);
+    const bool few = plan.splits <= 8;
+    if (bf16) few ? launch_join<__nv_bfloat16, 1>(a, st) : launch_join<__nv_bfloat16, 4>(a, st);
+    else few ? launch_join<float, 1>(a, st) : launch_join<float, 4>(a, st);
   }
 }
 

@@ -121,10 +121,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 2 + x); };      // P_X of tile j is
   auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };
   auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 6 + x); };      // its first 64 positions are
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 8));
+  auto q_full = [&](int x) { return bar_base + 8u * (2 * SR + 8 + x); };      // Q_X is in shared memory
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 10));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   volatile uint32_t* odd_flag = tmem_slot + 2;      // a value that is not finite was taken out of a tile
-  static_assert(8 * (2 * SR + 8) + 12 <= C::kBarBytes, "barrier area");
+  static_assert(8 * (2 * SR + 10) + 12 <= C::kBarBytes, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_wait();
@@ -134,7 +135,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   const int kvh = cta.kvh, b = cta.b;
   const PagedSeq sq = paged_seq(a.kv, b, kvh == 0 && cta.tile == 0 && cta.split == 0 && threadIdx.x == 0);
   const int G = a.G, R = sq.n * G, r0 = cta.tile * 256;
-  if (r0 >= R) return;
+  if (r0 >= R) return;                              // (the grid is made for the longest sequence)
   const int first_p = sq.len - sq.n;
   const bool two = r0 + 128 < R;                    // there are rows B
   const Visible v0 = visible(a, first_p + r0 / G, sq.len), v1 = visible(a, first_p + min(r0 + 255, R - 1) / G, sq.len);
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); }
+    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); mbar_init(q_full(x), 4); }
     *abort_flag = 0; *odd_flag = 0;
     mbar_fence_init();
     tma_prefetch_map(&tmK);
@@ -157,25 +158,6 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)), "r"(512));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-  }
-  // a softmax thread brings its own query row into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist
-  const int x = warp >= 8 ? 1 : 0;                  // row tile of a softmax thread
-  const int row = (warp & 3) * 32 + lane;           // = the TMEM lane this thread may read
-  bool live = false;
-  int tok = 0, head = 0, pos = 0;
-  Visible vis{0, 0};
-  if (warp >= 4) {
-    live = r0 + x * 128 + row < R;
-    const int rr = live ? r0 + x * 128 + row : r0;
-    tok = sq.row0 + rr / G; head = kvh * G + rr % G; pos = first_p + rr / G;
-    if (live) vis = visible(a, pos, sq.len);
-    const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (long long)tok * a.q_stride + (long long)head * HD);
-#pragma unroll
-    for (int c = 0; c < HD / 8; ++c) {
-      const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-      *reinterpret_cast<uint4*>(gen_base + x * C::kQBytes + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
-    }
-    fence_async();
   }
   tc_fence_before();
   __syncthreads();
@@ -234,7 +216,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         }
       };
       if (NT > 0) {
-        ok = slot_ready(0);
+        ok = slot_ready(0) && warp_wait_uniform(q_full(0), 0u, abort_flag) && (!two || warp_wait_uniform(q_full(1), 0u, abort_flag));
         if (ok) {
           tc_fence_after();
           issue_s(0, 0);
@@ -269,6 +251,22 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     // ------------------------------------------------------------------ softmax, one thread per row
+    // a thread brings its own query row into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist, while the first tiles are on their way
+    const int x = warp >= 8 ? 1 : 0;                  // row tile of a softmax thread
+    const int row = (warp & 3) * 32 + lane;           // = the TMEM lane this thread may read
+    const bool live = r0 + x * 128 + row < R;
+    const int rr = live ? r0 + x * 128 + row : r0;
+    const int tok = sq.row0 + rr / G, head = kvh * G + rr % G, pos = first_p + rr / G;
+    const Visible vis = live ? visible(a, pos, sq.len) : Visible{0, 0};
+    const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (long long)tok * a.q_stride + (long long)head * HD);
+#pragma unroll
+    for (int c = 0; c < HD / 8; ++c) {
+      const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(gen_base + x * C::kQBytes + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+    }
+    fence_async();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(q_full(x));
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem_base + lane_addr + 128u * x, t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
     const float sc = a.scale * 1.4426950408889634f;       // scores in base 2
@@ -439,6 +437,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
       const bool odd = edges && *odd_flag, none = l_run == 0.f;
       const float inv = none ? 0.f : 1.f / l_run;
       const long long at = ((long long)cta.split * a.kv.rows + tok) * a.Hq + head;
+      // where this thread's row goes (elements of the output or of the parts), -1: nowhere
+      const long long mine = !live || (a.splits > 1 && none) ? -1 : a.splits > 1 ? at * HD : (long long)tok * a.out_stride + (long long)head * HD;
+      float4* turn = reinterpret_cast<float4*>(gen_base + x * C::kQBytes) + (warp & 3) * 256;
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {
         float ov[32];
@@ -460,24 +461,19 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
           }
           __syncwarp();
         }
-        if (live) {
-          if (none) {
+        // turned in shared memory, where Q_X was, so that neighbouring lanes have neighbouring pieces of a row (each its own row's: 2,800 cycles)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) ov[i] = 0.f;
-          }
-          if (a.splits > 1) {
-            float4* op = reinterpret_cast<float4*>(a.part_o + at * HD + 32 * c);
-            if (!none)
+        for (int i = 0; i < 8; ++i)
+          turn[lane * 8 + (i ^ (lane & 7))] = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(ov[4 * i] * inv, ov[4 * i + 1] * inv, ov[4 * i + 2] * inv, ov[4 * i + 3] * inv);
+        __syncwarp();
 #pragma unroll
-              for (int i = 0; i < 8; ++i) op[i] = make_float4(ov[4 * i] * inv, ov[4 * i + 1] * inv, ov[4 * i + 2] * inv, ov[4 * i + 3] * inv);
-          } else {
-            uint4* op = reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + (long long)tok * a.out_stride + (long long)head * HD + 32 * c);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const uint2 lo = pack_bf16x4(ov[8 * u] * inv, ov[8 * u + 1] * inv, ov[8 * u + 2] * inv, ov[8 * u + 3] * inv);
-              const uint2 hi = pack_bf16x4(ov[8 * u + 4] * inv, ov[8 * u + 5] * inv, ov[8 * u + 6] * inv, ov[8 * u + 7] * inv);
-              op[u] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-            }
+        for (int i = 0; i < 8; ++i) {
+          const int r = 4 * i + (lane >> 3);         // row of the warp's 32
+          const float4 v = turn[r * 8 + ((lane & 7) ^ (r & 7))];
+          const long long to = __shfl_sync(0xffffffffu, mine, r);
+          if (to >= 0) {
+            if (a.splits > 1) *reinterpret_cast<float4*>(a.part_o + to + 32 * c + 4 * (lane & 7)) = v;
+            else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + to + 32 * c + 4 * (lane & 7)) = pack_bf16x4(v.x, v.y, v.z, v.w);
           }
         }
         __syncwarp();
