@@ -170,25 +170,33 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
       // ------------------------------------------------------------------ copies: K_0, V_0, K_1, V_1, ... through one ring
       const uint32_t leader = elect_one();
       const int nb = kPosP / box_rows;
-      auto look_up = [&](int tile) { return lane < nb ? page_of(a.kv, b, tile * kPosP + lane * box_rows, box_rows, u_lo, u_hi) : 0; };
-      int page = NT > 0 ? look_up(t_begin) : 0, i = 0, s = 0;
+      // the boxes of all tiles are numbered through; a lane has the page of one in 32 of them, looked up 32 boxes ahead
+      auto look_up = [&](int box) {
+        box += lane;
+        return box < NT * nb ? page_of(a.kv, b, t_begin * kPosP + box * box_rows, box_rows, u_lo, u_hi) : 0;
+      };
+      int page = look_up(0), next = look_up(32), y0 = t_begin * kPosP % a.kv.page_size, i = 0, s = 0;
       uint32_t round = 0;
       bool ok = true;
       for (int t = 0; t < NT && ok; ++t) {
-        const int next = t + 1 < NT ? look_up(t_begin + t + 1) : 0;
-        const int p0 = (t_begin + t) * kPosP;
+        const int first = t * nb;                    // (nb divides 32)
+        if (t > 0 && (first & 31) == 0) { page = next; next = look_up(first + 32); }
+        int y = 0;
         for (int kv = 0; kv < 2; ++kv, ++i) {
           if (!warp_wait_uniform(empty_bar(s), round ^ 1u, abort_flag)) { ok = false; break; }
           mbar_expect_tx_if(full_bar(s), C::kTileBytes, leader);
+          y = y0;
           for (int n = 0; n < nb; ++n) {
-            const int pg = __shfl_sync(0xffffffffu, page, n), y = (p0 + n * box_rows) % a.kv.page_size;
+            const int pg = __shfl_sync(0xffffffffu, page, (first + n) & 31);
 #pragma unroll
             for (int h = 0; h < NH; ++h)
               tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y, kvh, pg, full_bar(s), leader);
+            y += box_rows;
+            if (y >= a.kv.page_size) y -= a.kv.page_size;
           }
           if (++s == SR) { s = 0; round ^= 1u; }
         }
-        page = next;
+        y0 = y;
       }
       if (!ok && lane == 0) {                        // the copies in flight land before the CTA's memory goes away
         *abort_flag = 1;
