@@ -8,6 +8,8 @@
 //   than 8 in log2, when O is rescaled in TMEM), base-2 exponentials, P as bf16 over the columns that its scores came from;
 //   O_X += P V with P read from TMEM; S_X of the next tile is issued right behind it.
 // While one tile's rows go through softmax, the tensor core runs the other tile's products: P_A V, S_A', P_B V, S_B', ...
+// ONE, of calls of at most 128 rows: rows A have both buffers of S, so S of the next tile is there before the softmax of this one ends (148 such CTAs, heads of
+// 128 over 16k positions: 379 us, the rate of the memory; 459 with one buffer).  With 256 rows a third buffer made A and B fall into step: 977 us for 919.
 // What a row does not see has no part in its sums (see paged_attention_tc.cu); a thread looks after one position of a tile on the edge.
 // Waits are bounded as everywhere.
 #include <math.h>
@@ -106,7 +108,7 @@ constexpr float kTanh[5] = {0.99999994f, -0.33332309f, 0.13310173f, -0.052101482
 // FORM, a sum of: scores capped; scores biased by their distance (or a scale that is not positive).  0: neither.
 enum { kCap = 1, kBias = 2 };
 
-template <int HD, int FORM>
+template <int HD, int FORM, bool ONE>
 __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                                                                       PagedAttnArgs a, int row_tiles, int box_rows) {
   using C = UCfg<HD>;
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   auto empty_bar = [&](int s) { return bar_base + 8u * (SR + s); };
   auto s_full = [&](int x) { return bar_base + 8u * (2 * SR + x); };          // S_X of tile j is in TMEM (and O_X holds the tiles before it)
   auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 2 + x); };      // P_X of tile j is
-  auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };
+  auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };      // (ONE: O_A holds tile j, x = j % 2)
   auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 6 + x); };      // its first 64 positions are
   auto q_full = [&](int x) { return bar_base + 8u * (2 * SR + 8 + x); };      // Q_X is in shared memory
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 10));
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   const int G = a.G, R = sq.n * G, r0 = cta.tile * 256;
   if (r0 >= R) return;                              // (the grid is made for the longest sequence)
   const int first_p = sq.len - sq.n;
-  const bool two = r0 + 128 < R;                    // there are rows B
+  const bool two = !ONE && r0 + 128 < R;            // there are rows B
   const Visible v0 = visible(a, first_p + r0 / G, sq.len), v1 = visible(a, first_p + min(r0 + 255, R - 1) / G, sq.len);
   const int u_lo = v0.lo, u_hi = v1.hi, c_lo = v1.lo, c_hi = v0.hi;      // what some of the rows see; what all of them see
   int t_begin = u_lo / kPosP, t_end = (u_hi + kPosP - 1) / kPosP;
@@ -146,6 +148,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
     t_end = min(t_end, (cta.split + 1) * (a.split_tiles / 2));
   }
   const int NT = max(0, t_end - t_begin);
+  // ONE: the columns of S_B are a second buffer for rows A, tile j uses x = j % 2, and S of the next tile is there before the softmax of this one ends.
+  // K is then needed two tiles ahead of V, otherwise one; the ring's order is K_0 .. K_{lead - 1}, V_0, K_lead, V_1, K_{lead + 1}, ...
+  constexpr int lead = ONE ? 2 : 1;
+  auto k_at = [&](int t) { return t < lead ? t : 2 * t - lead + 1; };
+  auto v_at = [&](int t) { return lead + 2 * t; };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
@@ -175,82 +182,112 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         box += lane;
         return box < NT * nb ? page_of(a.kv, b, t_begin * kPosP + box * box_rows, box_rows, u_lo, u_hi) : 0;
       };
-      int page = look_up(0), next = look_up(32), y0 = t_begin * kPosP % a.kv.page_size, i = 0, s = 0;
-      uint32_t round = 0;
-      bool ok = true;
-      for (int t = 0; t < NT && ok; ++t) {
-        const int first = t * nb;                    // (nb divides 32)
-        if (t > 0 && (first & 31) == 0) { page = next; next = look_up(first + 32); }
-        int y = 0;
-        for (int kv = 0; kv < 2; ++kv, ++i) {
-          if (!warp_wait_uniform(empty_bar(s), round ^ 1u, abort_flag)) { ok = false; break; }
-          mbar_expect_tx_if(full_bar(s), C::kTileBytes, leader);
-          y = y0;
-          for (int n = 0; n < nb; ++n) {
-            const int pg = __shfl_sync(0xffffffffu, page, (first + n) & 31);
+      // (of each of K and V: the pages of its present 32 boxes and of the next, its place in its page)
+      int page[2], next[2], y[2], last = -1;
+      page[0] = page[1] = look_up(0);
+      next[0] = next[1] = look_up(32);
+      y[0] = y[1] = t_begin * kPosP % a.kv.page_size;
+      auto bring = [&](int kv, int t, int i) {
+        const int s = i % SR, first = t * nb;        // (nb divides 32)
+        if (i >= SR && !warp_wait_uniform(empty_bar(s), (uint32_t)(i / SR - 1) & 1u, abort_flag)) return false;
+        if (t > 0 && (first & 31) == 0) { page[kv] = next[kv]; next[kv] = look_up(first + 32); }
+        mbar_expect_tx_if(full_bar(s), C::kTileBytes, leader);
+        for (int n = 0; n < nb; ++n) {
+          const int pg = __shfl_sync(0xffffffffu, page[kv], (first + n) & 31);
 #pragma unroll
-            for (int h = 0; h < NH; ++h)
-              tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y, kvh, pg, full_bar(s), leader);
-            y += box_rows;
-            if (y >= a.kv.page_size) y -= a.kv.page_size;
-          }
-          if (++s == SR) { s = 0; round ^= 1u; }
+          for (int h = 0; h < NH; ++h)
+            tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y[kv], kvh, pg, full_bar(s), leader);
+          y[kv] += box_rows;
+          if (y[kv] >= a.kv.page_size) y[kv] -= a.kv.page_size;
         }
-        y0 = y;
+        last = i;
+        return true;
+      };
+      bool ok = true;
+      for (int t = 0; t < min(lead, NT) && ok; ++t) ok = bring(0, t, k_at(t));
+      for (int t = 0; t < NT && ok; ++t) {
+        ok = bring(1, t, v_at(t));
+        if (ok && t + lead < NT) ok = bring(0, t + lead, k_at(t + lead));
       }
       if (!ok && lane == 0) {                        // the copies in flight land before the CTA's memory goes away
         *abort_flag = 1;
-        for (int j = max(0, i - SR); j < i; ++j) mbar_wait(full_bar(j % SR), (j / SR) & 1);
+        for (int j = max(0, last - SR + 1); j <= last; ++j) mbar_wait(full_bar(j % SR), (j / SR) & 1);
       }
     } else if (warp == 1) {
       // ------------------------------------------------------------------ products
       const uint32_t leader = elect_one();
       bool ok = true;
       auto slot_ready = [&](int i) { return warp_wait_uniform(full_bar(i % SR), (uint32_t)(i / SR) & 1u, abort_flag); };
-      auto issue_s = [&](int xx, int j) {            // S_X = Q_X K_j^T
-        const uint32_t kt = ring + (2 * j % SR) * C::kTileBytes, qt = base + xx * C::kQBytes;
+      auto issue_s = [&](int u, int xx, int i) {     // S of buffer u = Q_X K^T, K at place i of the ring's order
+        const uint32_t kt = ring + (i % SR) * C::kTileBytes, qt = base + xx * C::kQBytes;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
-          tc_mma(tmem_base + 128u * xx, smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
+          tc_mma(tmem_base + 128u * u, smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
                  C::kIdescS, ks > 0 ? 1u : 0u, leader);
+        tc_commit_if(s_full(u), leader);
       };
-      auto issue_pv = [&](int xx, int j, int half) {      // O_X += P_X V_j, 64 of the positions
-        const uint32_t vt = ring + ((2 * j + 1) % SR) * C::kTileBytes;
+      auto issue_pv = [&](int u, int xx, int i, int half, bool first) {      // O_X += P V, P of buffer u, 64 of the positions
+        const uint32_t vt = ring + (i % SR) * C::kTileBytes;
 #pragma unroll
         for (int kk = 0; kk < kPosP / 32; ++kk) {
           const int ks = half * (kPosP / 32) + kk;
-          mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + 128u * xx + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
-                     j > 0 || ks > 0 ? 1u : 0u, leader);
+          mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + 128u * u + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
+                     !first || ks > 0 ? 1u : 0u, leader);
         }
       };
-      if (NT > 0) {
-        ok = slot_ready(0) && warp_wait_uniform(q_full(0), 0u, abort_flag) && (!two || warp_wait_uniform(q_full(1), 0u, abort_flag));
-        if (ok) {
-          tc_fence_after();
-          issue_s(0, 0);
-          tc_commit_if(s_full(0), leader);
-          if (two) { issue_s(1, 0); tc_commit_if(s_full(1), leader); }
-          tc_commit_if(empty_bar(0), leader);        // K_0 may be overwritten
+      auto add_pv = [&](int u, int xx, int j, uint32_t parity) {             // O_X += P V of tile j, as P comes
+        if (!warp_wait_uniform(p_half(u), parity, abort_flag)) return false;
+        tc_fence_after();
+        issue_pv(u, xx, v_at(j), 0, j == 0);
+        if (!warp_wait_uniform(p_full(u), parity, abort_flag)) return false;
+        tc_fence_after();
+        issue_pv(u, xx, v_at(j), 1, false);
+        return true;
+      };
+      if constexpr (!ONE) {
+        if (NT > 0) {
+          ok = slot_ready(0) && warp_wait_uniform(q_full(0), 0u, abort_flag) && (!two || warp_wait_uniform(q_full(1), 0u, abort_flag));
+          if (ok) {
+            tc_fence_after();
+            issue_s(0, 0, 0);
+            if (two) issue_s(1, 1, 0);
+            tc_commit_if(empty_bar(0), leader);      // K_0 may be overwritten
+          }
         }
-      }
-      for (int j = 0; j < NT && ok; ++j) {
-        const bool more = j + 1 < NT;
-        if (!slot_ready(2 * j + 1) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
-        for (int xx = 0; xx < (two ? 2 : 1); ++xx) {
-          const bool last = xx == 1 || !two;
-          if (!warp_wait_uniform(p_half(xx), (uint32_t)j & 1u, abort_flag)) { ok = false; break; }
+        for (int j = 0; j < NT && ok; ++j) {
+          const bool more = j + 1 < NT;
+          if (!slot_ready(2 * j + 1) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
+          for (int xx = 0; xx < (two ? 2 : 1); ++xx) {
+            const bool last = xx == 1 || !two;
+            ok = add_pv(xx, xx, j, (uint32_t)j & 1u);
+            if (!ok) break;
+            if (last) tc_commit_if(empty_bar((2 * j + 1) % SR), leader);
+            if (more) {                              // (behind P_X V_j, whose P lies where this goes: a CTA's products run in order)
+              issue_s(xx, xx, 2 * j + 2);
+              if (last) tc_commit_if(empty_bar((2 * j + 2) % SR), leader);
+            } else {
+              tc_commit_if(o_full(xx), leader);
+            }
+          }
+        }
+      } else {
+        if (NT > 0) ok = warp_wait_uniform(q_full(0), 0u, abort_flag);
+        for (int j = 0; j < min(2, NT) && ok; ++j) {
+          ok = slot_ready(j);
+          if (!ok) break;
           tc_fence_after();
-          issue_pv(xx, j, 0);
-          if (!warp_wait_uniform(p_full(xx), (uint32_t)j & 1u, abort_flag)) { ok = false; break; }
-          tc_fence_after();
-          issue_pv(xx, j, 1);
-          if (last) tc_commit_if(empty_bar((2 * j + 1) % SR), leader);
+          issue_s(j, 0, j);
+          tc_commit_if(empty_bar(j), leader);
+        }
+        for (int j = 0; j < NT && ok; ++j) {
+          const bool more = j + 2 < NT;
+          ok = slot_ready(v_at(j)) && (!more || slot_ready(k_at(j + 2))) && add_pv(j & 1, 0, j, (uint32_t)(j >> 1) & 1u);
+          if (!ok) break;
+          tc_commit_if(o_full(j & 1), leader);
+          tc_commit_if(empty_bar(v_at(j) % SR), leader);
           if (more) {
-            issue_s(xx, j + 1);                      // (behind P_X V_j, whose P lies where this goes: a CTA's products run in order)
-            tc_commit_if(s_full(xx), leader);
-            if (last) tc_commit_if(empty_bar((2 * j + 2) % SR), leader);
-          } else {
-            tc_commit_if(o_full(xx), leader);
+            issue_s(j & 1, 0, k_at(j + 2));
+            tc_commit_if(empty_bar(k_at(j + 2) % SR), leader);
           }
         }
       }
@@ -276,7 +313,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
     __syncwarp();
     if (lane == 0) mbar_arrive(q_full(x));
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem_base + lane_addr + 128u * x, t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
+    const uint32_t t_o = tmem_base + lane_addr + C::kColO + (uint32_t)(HD * x);
     const float sc = a.scale * 1.4426950408889634f;       // scores in base 2
     const float slope = (FORM & kBias) && a.slopes ? a.slopes[head] * 1.4426950408889634f : 0.f;
     // capped: cap2 tanh(s inv_cap) = s (k_0 + k_1 s^2 + ...) while no score of the warp's rows is beyond kTanhRange
@@ -290,7 +327,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
       for (int j = 0; j < NT; ++j) {
         const int p0 = (t_begin + j) * kPosP;
         const bool edge = j < j_lo || j >= j_hi;
-        ok = warp_wait_uniform(s_full(x), (uint32_t)j & 1u, abort_flag);
+        const int u = ONE ? j & 1 : x;               // its buffer of S
+        const uint32_t t_s = tmem_base + lane_addr + 128u * u;
+        ok = warp_wait_uniform(s_full(u), (uint32_t)(ONE ? j >> 1 : j) & 1u, abort_flag);
         if (!ok) break;
         tc_fence_after();
         float sv[kPosP];
@@ -372,6 +411,11 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         const float corr = raise ? ex2(m_ref - m_safe) : 1.f;
         m_ref = m_new;
         if (j > 0 && __any_sync(0xffffffffu, raise)) {      // rescale O (its products so far are complete: S_j was issued behind them)
+          if constexpr (ONE) {                       // (or, with two buffers, are waited for)
+            ok = warp_wait_uniform(o_full(u ^ 1), (uint32_t)((j - 1) >> 1) & 1u, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+          }
 #pragma unroll 1
           for (int c = 0; c < HD / 32; ++c) {
             uint32_t ov[32];
@@ -386,9 +430,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         if (edge) {
           // this thread's position of the V tile: zeros where no row of the CTA sees it; where some do not, finite values stay
           edges = true;
-          ok = warp_wait_uniform(full_bar((2 * j + 1) % SR), (uint32_t)((2 * j + 1) / SR) & 1u, abort_flag);
+          ok = warp_wait_uniform(full_bar(v_at(j) % SR), (uint32_t)(v_at(j) / SR) & 1u, abort_flag);
           if (!ok) break;
-          uint8_t* vg = gen_base + (ring - base) + ((2 * j + 1) % SR) * C::kTileBytes + row * 128;
+          uint8_t* vg = gen_base + (ring - base) + (v_at(j) % SR) * C::kTileBytes + row * 128;
           const int p = p0 + row;
           if (p < c_lo || p >= c_hi) {               // (neighbouring threads take a row's pieces in different orders: 16 bytes of each of 8 rows are 128 of the banks)
             const bool unseen = p < u_lo || p >= u_hi;
@@ -422,7 +466,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_half(x));
+            if (lane == 0) mbar_arrive(p_half(u));
           }
         }
         float rs_lo, rs_hi;
@@ -431,10 +475,10 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(x));
+        if (lane == 0) mbar_arrive(p_full(u));
       }
       if (ok && NT > 0) {
-        ok = warp_wait_uniform(o_full(x), 0u, abort_flag);
+        ok = !ONE ? warp_wait_uniform(o_full(x), 0u, abort_flag) : warp_wait_uniform(o_full((NT - 1) & 1), (uint32_t)((NT - 1) >> 1) & 1u, abort_flag);
         tc_fence_after();
       }
     }
@@ -503,32 +547,32 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 }
 
 // The softmax warpgroups take more registers a thread and leave the other fewer: the launch has to have them all (else they would wait).
-template <int HD, int FORM>
+template <int HD, int FORM, bool ONE>
 bool registers_add_up() {
   cudaFuncAttributes at{};
-  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM>) == cudaSuccess && at.numRegs * kThreadsP >= kRegsRest * 128 + kRegsSoftmax * 256;
+  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM, ONE>) == cudaSuccess && at.numRegs * kThreadsP >= kRegsRest * 128 + kRegsSoftmax * 256;
 }
 
-template <int HD, int FORM>
+template <int HD, int FORM, bool ONE>
 bool launch(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, int box_rows, cudaStream_t st) {
   using C = UCfg<HD>;
-  static const bool fits = registers_add_up<HD, FORM>();
+  static const bool fits = registers_add_up<HD, FORM, ONE>();
   if (!fits) return false;
   static PerDeviceOnce configured;
-  configured.run([] { cudaFuncSetAttribute(paged_attn_umma_kernel<HD, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes); });
+  configured.run([] { cudaFuncSetAttribute(paged_attn_umma_kernel<HD, FORM, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes); });
   const int row_tiles = (int)(((long long)a.kv.max_new * a.G + 255) / 256);
-  launch_pdl(paged_attn_umma_kernel<HD, FORM>, dim3((unsigned)((long long)a.kv.Hkv * row_tiles * a.splits * a.kv.batch)), dim3(kThreadsP), C::kSmemBytes, st, tk, tv, a,
+  launch_pdl(paged_attn_umma_kernel<HD, FORM, ONE>, dim3((unsigned)((long long)a.kv.Hkv * row_tiles * a.splits * a.kv.batch)), dim3(kThreadsP), C::kSmemBytes, st, tk, tv, a,
              row_tiles, box_rows);
   return true;
 }
 
-template <int HD>
+template <int HD, bool ONE>
 bool launch_form(const PagedAttnArgs& a, int form, const CUtensorMap& tk, const CUtensorMap& tv, int box, cudaStream_t st) {
   switch (form) {
-    case 0: return launch<HD, 0>(a, tk, tv, box, st);
-    case kCap: return launch<HD, kCap>(a, tk, tv, box, st);
-    case kBias: return launch<HD, kBias>(a, tk, tv, box, st);
-    default: return launch<HD, kCap + kBias>(a, tk, tv, box, st);
+    case 0: return launch<HD, 0, ONE>(a, tk, tv, box, st);
+    case kCap: return launch<HD, kCap, ONE>(a, tk, tv, box, st);
+    case kBias: return launch<HD, kBias, ONE>(a, tk, tv, box, st);
+    default: return launch<HD, kCap + kBias, ONE>(a, tk, tv, box, st);
   }
 }
 
@@ -540,8 +584,9 @@ bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
   const int box = paged_box_rows(a.kv.page_size);
   if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
   const int form = (a.softcap > 0.f ? kCap : 0) + (a.slopes || !(a.scale > 0.f) ? kBias : 0);
-  if (a.kv.hd == 64) return launch_form<64>(a, form, tk, tv, box, st);
-  return launch_form<128>(a, form, tk, tv, box, st);
+  const bool one = (long long)a.kv.max_new * a.G <= 128;
+  if (a.kv.hd == 64) return one ? launch_form<64, true>(a, form, tk, tv, box, st) : launch_form<64, false>(a, form, tk, tv, box, st);
+  return one ? launch_form<128, true>(a, form, tk, tv, box, st) : launch_form<128, false>(a, form, tk, tv, box, st);
 }
 
 }  // namespace nz
