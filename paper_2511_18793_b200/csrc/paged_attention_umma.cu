@@ -25,21 +25,25 @@ namespace {
 using namespace gemm_detail;
 using namespace paged_detail;
 
-constexpr int kPosP = 128;         // positions per tile
-constexpr int kThreadsP = 384;     // warps 0 to 3: copies, products, two idle; 4 to 7: rows A; 8 to 11: rows B
-constexpr int kRegsRest = 88, kRegsSoftmax = 208;       // registers a thread; together what 384 threads of 168 have
 constexpr float kRaise = 8.f;
 
-template <int HD> struct UCfg {
+// NX: row tiles of a CTA (1, 2, 4)
+template <int HD, int NX> struct UCfg {
+  static constexpr int kPos = NX == 4 ? 64 : 128;              // positions per tile
+  static constexpr int kGroups = NX == 4 ? 4 : 2;              // softmax warpgroups (of one row tile the second is idle)
+  static constexpr int kThreads = 128 + 128 * kGroups;         // warps 0 to 3: copies, products, edges; from 4: the row tiles, four each
+  // registers a thread; together what the threads have at the launch (168 of 384, 96 of 640)
+  static constexpr int kRegsRest = NX == 4 ? 64 : 88, kRegsSoftmax = NX == 4 ? 104 : 208;
   static constexpr int kQBytes = 128 * HD * 2;                 // one row tile
-  static constexpr int kTileBytes = kPosP * HD * 2;            // one K or V tile
-  static constexpr int kSlots = HD == 128 ? 5 : 8;
-  static constexpr int kBarBytes = 256;
-  static constexpr int kSmemBytes = 2 * kQBytes + kSlots * kTileBytes + kBarBytes + 1024;
-  static constexpr uint32_t kColO = 256;                       // S_A 0, S_B 128, O_A 256, O_B 256 + HD
-  static constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kPosP >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+  static constexpr int kTileBytes = kPos * HD * 2;             // one K or V tile
+  static constexpr int kSlots = NX == 4 ? 16 : HD == 128 ? 5 : 8;
+  static constexpr int kBarBytes = 512;
+  static constexpr int kSmemBytes = kGroups * kQBytes + kSlots * kTileBytes + kBarBytes + 1024;
+  static constexpr uint32_t kColO = 256;                       // TMEM: kPos columns of S for each row tile (of one: two buffers), then O of each
+  static constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kPos >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
   static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) /* B is N-major */ | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
   static_assert(kSmemBytes <= 227 * 1024 && 2 * kSmemBytes > 227 * 1024, "one CTA per SM");
+  static_assert(kColO + kGroups * HD <= 512, "TMEM");
 };
 
 __device__ __forceinline__ void mma_a_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate, uint32_t leader) {
@@ -108,26 +112,31 @@ constexpr float kTanh[5] = {0.99999994f, -0.33332309f, 0.13310173f, -0.052101482
 // FORM, a sum of: scores capped; scores biased by their distance (or a scale that is not positive).  0: neither.
 enum { kCap = 1, kBias = 2 };
 
-template <int HD, int FORM, bool ONE>
-__global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+template <int HD, int FORM, int NX>
+__global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                                                                       PagedAttnArgs a, int row_tiles, int box_rows) {
-  using C = UCfg<HD>;
-  constexpr int SR = C::kSlots, NH = HD / 64, KS = HD / 16;
+  using C = UCfg<HD, NX>;
+  constexpr int SR = C::kSlots, NH = HD / 64, KS = HD / 16, kPosP = C::kPos;
+  constexpr bool ONE = NX == 1;
+  constexpr bool kHalves = NX < 4;      // P V begins when half of P is there
+  constexpr bool kTurns = NX == 2 && (FORM & kCap) != 0;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t ring = base + 2 * C::kQBytes, bar_base = ring + SR * C::kTileBytes;
+  const uint32_t ring = base + C::kGroups * C::kQBytes, bar_base = ring + SR * C::kTileBytes;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (SR + s); };
   auto s_full = [&](int x) { return bar_base + 8u * (2 * SR + x); };          // S_X of tile j is in TMEM (and O_X holds the tiles before it)
-  auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 2 + x); };      // P_X of tile j is
-  auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };      // (ONE: O_A holds tile j, x = j % 2)
-  auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 6 + x); };      // its first 64 positions are
-  auto q_full = [&](int x) { return bar_base + 8u * (2 * SR + 8 + x); };      // Q_X is in shared memory
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 10));
+  auto p_full = [&](int x) { return bar_base + 8u * (2 * SR + 4 + x); };      // P_X of tile j is
+  auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 8 + x); };      // (ONE: O_A holds tile j, x = j % 2)
+  auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 12 + x); };      // its first 64 positions are
+  auto q_full = [&](int x) { return bar_base + 8u * (2 * SR + 16 + x); };      // Q_X is in shared memory
+  auto exp_turn = [&](int x, int w) { return bar_base + 8u * (2 * SR + 20 + 4 * x + w); };      // warp w of rows x may go through its exponentials
+  const uint32_t edge_bar = bar_base + 8u * (2 * SR + 28), clean_bar = edge_bar + 8u;      // the next V tile on the edge is in its slot; what no row sees is out of it
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 30));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   volatile uint32_t* odd_flag = tmem_slot + 2;      // a value that is not finite was taken out of a tile
-  static_assert(8 * (2 * SR + 10) + 12 <= C::kBarBytes, "barrier area");
+  static_assert(8 * (2 * SR + 30) + 12 <= C::kBarBytes, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_wait();
@@ -136,18 +145,22 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   cta.tile = row_tiles - 1 - cta.tile;              // the rows that see the most context go first
   const int kvh = cta.kvh, b = cta.b;
   const PagedSeq sq = paged_seq(a.kv, b, kvh == 0 && cta.tile == 0 && cta.split == 0 && threadIdx.x == 0);
-  const int G = a.G, R = sq.n * G, r0 = cta.tile * 256;
+  const int G = a.G, R = sq.n * G, r0 = cta.tile * (128 * C::kGroups);
   if (r0 >= R) return;                              // (the grid is made for the longest sequence)
   const int first_p = sq.len - sq.n;
-  const bool two = !ONE && r0 + 128 < R;            // there are rows B
-  const Visible v0 = visible(a, first_p + r0 / G, sq.len), v1 = visible(a, first_p + min(r0 + 255, R - 1) / G, sq.len);
+  const int nx = ONE ? 1 : min(NX, (R - r0 + 127) / 128);      // row tiles that there are
+  const Visible v0 = visible(a, first_p + r0 / G, sq.len), v1 = visible(a, first_p + min(r0 + 128 * C::kGroups - 1, R - 1) / G, sq.len);
   const int u_lo = v0.lo, u_hi = v1.hi, c_lo = v1.lo, c_hi = v0.hi;      // what some of the rows see; what all of them see
   int t_begin = u_lo / kPosP, t_end = (u_hi + kPosP - 1) / kPosP;
   if (a.splits > 1) {
-    t_begin = max(t_begin, cta.split * (a.split_tiles / 2));
-    t_end = min(t_end, (cta.split + 1) * (a.split_tiles / 2));
+    t_begin = max(t_begin, cta.split * (a.split_tiles * kAttnTile / kPosP));
+    t_end = min(t_end, (cta.split + 1) * (a.split_tiles * kAttnTile / kPosP));
   }
   const int NT = max(0, t_end - t_begin);
+  // The j-th tile of the CTA's share.  With a bias by distance the near positions, whose scores are large, go first: else the reference maximum would be raised tile by tile.
+  constexpr bool kBack = (FORM & kBias) != 0;
+  auto tile_at = [&](int j) { return kBack ? t_end - 1 - j : t_begin + j; };
+  auto on_edge = [&](int tile) { return tile * kPosP < c_lo || (tile + 1) * kPosP > c_hi; };      // some of the rows do not see all of it
   // ONE: the columns of S_B are a second buffer for rows A, tile j uses x = j % 2, and S of the next tile is there before the softmax of this one ends.
   // K is then needed two tiles ahead of V, otherwise one; the ring's order is K_0 .. K_{lead - 1}, V_0, K_lead, V_1, K_{lead + 1}, ...
   constexpr int lead = ONE ? 2 : 1;
@@ -156,7 +169,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int x = 0; x < 2; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); mbar_init(q_full(x), 4); }
+    for (int x = 0; x < 4; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); mbar_init(q_full(x), 4); }
+    for (int i = 0; i < 8; ++i) mbar_init(exp_turn(i >> 2, i & 3), 1);
+    mbar_init(edge_bar, 1); mbar_init(clean_bar, 2);
     *abort_flag = 0; *odd_flag = 0;
     mbar_fence_init();
     tma_prefetch_map(&tmK);
@@ -172,7 +187,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
   const uint32_t tmem_base = *tmem_slot;
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsRest));
     if (warp == 0) {
       // ------------------------------------------------------------------ copies: K_0, V_0, K_1, V_1, ... through one ring
       const uint32_t leader = elect_one();
@@ -180,25 +195,26 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
       // the boxes of all tiles are numbered through; a lane has the page of one in 32 of them, looked up 32 boxes ahead
       auto look_up = [&](int box) {
         box += lane;
-        return box < NT * nb ? page_of(a.kv, b, t_begin * kPosP + box * box_rows, box_rows, u_lo, u_hi) : 0;
+        const int j = box / nb;
+        return j < NT ? page_of(a.kv, b, tile_at(j) * kPosP + (box - j * nb) * box_rows, box_rows, u_lo, u_hi) : 0;
       };
-      // (of each of K and V: the pages of its present 32 boxes and of the next, its place in its page)
-      int page[2], next[2], y[2], last = -1;
+      // (of each of K and V: the pages of its present 32 boxes and of the next)
+      int page[2], next[2], last = -1;
       page[0] = page[1] = look_up(0);
       next[0] = next[1] = look_up(32);
-      y[0] = y[1] = t_begin * kPosP % a.kv.page_size;
       auto bring = [&](int kv, int t, int i) {
         const int s = i % SR, first = t * nb;        // (nb divides 32)
         if (i >= SR && !warp_wait_uniform(empty_bar(s), (uint32_t)(i / SR - 1) & 1u, abort_flag)) return false;
         if (t > 0 && (first & 31) == 0) { page[kv] = next[kv]; next[kv] = look_up(first + 32); }
+        int y = tile_at(t) * kPosP % a.kv.page_size;
         mbar_expect_tx_if(full_bar(s), C::kTileBytes, leader);
         for (int n = 0; n < nb; ++n) {
           const int pg = __shfl_sync(0xffffffffu, page[kv], (first + n) & 31);
 #pragma unroll
           for (int h = 0; h < NH; ++h)
-            tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y[kv], kvh, pg, full_bar(s), leader);
-          y[kv] += box_rows;
-          if (y[kv] >= a.kv.page_size) y[kv] -= a.kv.page_size;
+            tma_load_4d_if(ring + s * C::kTileBytes + h * (kPosP * 128) + n * box_rows * 128, kv ? &tmV : &tmK, h * 64, y, kvh, pg, full_bar(s), leader);
+          y += box_rows;
+          if (y >= a.kv.page_size) y -= a.kv.page_size;
         }
         last = i;
         return true;
@@ -222,7 +238,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         const uint32_t kt = ring + (i % SR) * C::kTileBytes, qt = base + xx * C::kQBytes;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
-          tc_mma(tmem_base + 128u * u, smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
+          tc_mma(tmem_base + (uint32_t)(kPosP * u), smem_desc(qt + (ks >> 2) * (128 * 128) + (ks & 3) * 32), smem_desc(kt + (ks >> 2) * (kPosP * 128) + (ks & 3) * 32),
                  C::kIdescS, ks > 0 ? 1u : 0u, leader);
         tc_commit_if(s_full(u), leader);
       };
@@ -231,34 +247,43 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 #pragma unroll
         for (int kk = 0; kk < kPosP / 32; ++kk) {
           const int ks = half * (kPosP / 32) + kk;
-          mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + 128u * u + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
+          mma_a_tmem(tmem_base + C::kColO + (uint32_t)(HD * xx), tmem_base + (uint32_t)(kPosP * u) + 8u * ks, desc_nmajor(vt + ks * (16 * 128), kPosP * 128), C::kIdescPV,
                      !first || ks > 0 ? 1u : 0u, leader);
         }
       };
+      uint32_t edges = 0;
+      auto clean = [&](int j) {                      // (V is in its slot)
+        if (!on_edge(tile_at(j))) return true;
+        if (leader) mbar_arrive(edge_bar);
+        return warp_wait_uniform(clean_bar, edges++ & 1u, abort_flag);
+      };
       auto add_pv = [&](int u, int xx, int j, uint32_t parity) {             // O_X += P V of tile j, as P comes
-        if (!warp_wait_uniform(p_half(u), parity, abort_flag)) return false;
-        tc_fence_after();
-        issue_pv(u, xx, v_at(j), 0, j == 0);
+        if constexpr (kHalves) {
+          if (!warp_wait_uniform(p_half(u), parity, abort_flag)) return false;
+          tc_fence_after();
+          issue_pv(u, xx, v_at(j), 0, j == 0);
+        }
         if (!warp_wait_uniform(p_full(u), parity, abort_flag)) return false;
         tc_fence_after();
+        if constexpr (!kHalves) issue_pv(u, xx, v_at(j), 0, j == 0);
         issue_pv(u, xx, v_at(j), 1, false);
         return true;
       };
       if constexpr (!ONE) {
         if (NT > 0) {
-          ok = slot_ready(0) && warp_wait_uniform(q_full(0), 0u, abort_flag) && (!two || warp_wait_uniform(q_full(1), 0u, abort_flag));
+          ok = slot_ready(0);
+          for (int xx = 0; xx < nx && ok; ++xx) ok = warp_wait_uniform(q_full(xx), 0u, abort_flag);
           if (ok) {
             tc_fence_after();
-            issue_s(0, 0, 0);
-            if (two) issue_s(1, 1, 0);
+            for (int xx = 0; xx < nx; ++xx) issue_s(xx, xx, 0);
             tc_commit_if(empty_bar(0), leader);      // K_0 may be overwritten
           }
         }
         for (int j = 0; j < NT && ok; ++j) {
           const bool more = j + 1 < NT;
-          if (!slot_ready(2 * j + 1) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
-          for (int xx = 0; xx < (two ? 2 : 1); ++xx) {
-            const bool last = xx == 1 || !two;
+          if (!slot_ready(2 * j + 1) || !clean(j) || (more && !slot_ready(2 * j + 2))) { ok = false; break; }
+          for (int xx = 0; xx < nx; ++xx) {
+            const bool last = xx == nx - 1;
             ok = add_pv(xx, xx, j, (uint32_t)j & 1u);
             if (!ok) break;
             if (last) tc_commit_if(empty_bar((2 * j + 1) % SR), leader);
@@ -281,7 +306,7 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         }
         for (int j = 0; j < NT && ok; ++j) {
           const bool more = j + 2 < NT;
-          ok = slot_ready(v_at(j)) && (!more || slot_ready(k_at(j + 2))) && add_pv(j & 1, 0, j, (uint32_t)(j >> 1) & 1u);
+          ok = slot_ready(v_at(j)) && clean(j) && (!more || slot_ready(k_at(j + 2))) && add_pv(j & 1, 0, j, (uint32_t)(j >> 1) & 1u);
           if (!ok) break;
           tc_commit_if(o_full(j & 1), leader);
           tc_commit_if(empty_bar(v_at(j) % SR), leader);
@@ -292,12 +317,41 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         }
       }
       if (!ok && leader) *abort_flag = 1;
+    } else {
+      // ------------------------------------------------------------------ V tiles on the edge: zeros where no row of the CTA sees a position; where some do not, finite values stay
+      bool ok = true;
+      uint32_t edges = 0;
+      for (int j = 0; j < NT && ok; ++j) {
+        if (!on_edge(tile_at(j))) continue;
+        const int i = v_at(j), s = i % SR;
+        // (full_bar alone would not do: it may be phases behind or ahead of a warp that passes over the tiles between)
+        ok = warp_wait_uniform(edge_bar, edges & 1u, abort_flag) && warp_wait_uniform(full_bar(s), (uint32_t)(i / SR) & 1u, abort_flag);
+        if (!ok) break;
+        ++edges;
+        for (int row = threadIdx.x - 64; row < kPosP; row += 64) {
+          uint8_t* vg = gen_base + (ring - base) + s * C::kTileBytes + row * 128;
+          const int p = tile_at(j) * kPosP + row;
+          if (p >= c_lo && p < c_hi) continue;
+          const bool unseen = p < u_lo || p >= u_hi;
+#pragma unroll 8
+          for (int i = 0; i < HD / 8; ++i) {         // (neighbouring threads take a row's pieces in different orders: 16 bytes of each of 8 rows are 128 of the banks)
+            const int c = i ^ (row & 7);
+            uint4* at = reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4));
+            if (unseen) *at = make_uint4(0u, 0u, 0u, 0u);
+            else if (any_odd(*at)) { *at = without_odd(*at); *odd_flag = 1; }
+          }
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(clean_bar);
+      }
+      if (!ok && lane == 0) *abort_flag = 1;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
     // ------------------------------------------------------------------ softmax, one thread per row
     // a thread brings its own query row into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist, while the first tiles are on their way
-    const int x = warp >= 8 ? 1 : 0;                  // row tile of a softmax thread
+    const int x = (warp >> 2) - 1;                    // row tile of a softmax thread
     const int row = (warp & 3) * 32 + lane;           // = the TMEM lane this thread may read
     const bool live = r0 + x * 128 + row < R;
     const int rr = live ? r0 + x * 128 + row : r0;
@@ -319,16 +373,13 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
     // capped: cap2 tanh(s inv_cap) = s (k_0 + k_1 s^2 + ...) while no score of the warp's rows is beyond kTanhRange
     const float cap2 = (FORM & kCap) ? a.softcap * 1.4426950408889634f : 0.f, inv_cap = (FORM & kCap) ? a.scale / a.softcap : 0.f;
     const int pos_min = (FORM & kBias) ? __reduce_min_sync(0xffffffffu, pos) : 0;
-    // tiles [j_lo, j_hi) are seen whole by all rows of the CTA
-    const int j_lo = (c_lo + kPosP - 1) / kPosP - t_begin, j_hi = c_hi / kPosP - t_begin;
     float m_ref = -INFINITY, l_run = 0.f;
-    bool ok = true, edges = false;
-    if (x == 0 || two) {
+    bool ok = true;
+    if (x < nx) {
       for (int j = 0; j < NT; ++j) {
-        const int p0 = (t_begin + j) * kPosP;
-        const bool edge = j < j_lo || j >= j_hi;
+        const int p0 = tile_at(j) * kPosP;
         const int u = ONE ? j & 1 : x;               // its buffer of S
-        const uint32_t t_s = tmem_base + lane_addr + 128u * u;
+        const uint32_t t_s = tmem_base + lane_addr + (uint32_t)(kPosP * u);
         ok = warp_wait_uniform(s_full(u), (uint32_t)(ONE ? j >> 1 : j) & 1u, abort_flag);
         if (!ok) break;
         tc_fence_after();
@@ -344,9 +395,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
         if constexpr ((FORM & kCap) != 0) {
           float mb[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kPosP; c += 4)
+          for (int c = 0; c < kPosP; c += 8)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) mb[q] = fmaxf(mb[q], fabsf(sv[c + q]));
+            for (int q = 0; q < 4; ++q) mb[q] = max3(mb[q], fabsf(sv[c + 2 * q]), fabsf(sv[c + 2 * q + 1]));
           // (positions that nobody sees may be beyond; a NaN among them is not noticed here and stays one below)
           const float top = fmaxf(fmaxf(mb[0], mb[1]), fmaxf(mb[2], mb[3])) * fabsf(inv_cap), i2 = inv_cap * inv_cap, lead = cap2 * inv_cap;
           if (__all_sync(0xffffffffu, top <= kTanhNear)) {
@@ -387,13 +438,13 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(-slope, fabsf(rel - (float)c), sv[c]);
           }
         }
-        if (j < j_lo) {                              // (a tile is seldom on both edges)
+        if (p0 < c_lo) {                              // (a tile is seldom on both edges)
           const int from = vis.lo - p0;
 #pragma unroll
           for (int c = 0; c < kPosP; ++c)
             if (c < from) sv[c] = -INFINITY;
         }
-        if (j >= j_hi) {
+        if (p0 + kPosP > c_hi) {
           const int to = vis.hi - p0;
 #pragma unroll
           for (int c = 0; c < kPosP; ++c)
@@ -427,25 +478,13 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             tmem_st16(t_o + 32u * c + 16u, ov + 16);
           }
         }
-        if (edge) {
-          // this thread's position of the V tile: zeros where no row of the CTA sees it; where some do not, finite values stay
-          edges = true;
-          ok = warp_wait_uniform(full_bar(v_at(j) % SR), (uint32_t)(v_at(j) / SR) & 1u, abort_flag);
-          if (!ok) break;
-          uint8_t* vg = gen_base + (ring - base) + (v_at(j) % SR) * C::kTileBytes + row * 128;
-          const int p = p0 + row;
-          if (p < c_lo || p >= c_hi) {               // (neighbouring threads take a row's pieces in different orders: 16 bytes of each of 8 rows are 128 of the banks)
-            const bool unseen = p < u_lo || p >= u_hi;
-#pragma unroll 4
-            for (int i = 0; i < HD / 8; ++i) {
-              const int c = i ^ (row & 7);
-              uint4* at = reinterpret_cast<uint4*>(vg + (c >> 3) * (kPosP * 128) + ((c & 7) << 4));
-              if (unseen) *at = make_uint4(0u, 0u, 0u, 0u);
-              else if (any_odd(*at)) { *at = without_odd(*at); *odd_flag = 1; }
-            }
+        // Capped scores take as many instructions as the exponentials take cycles of their unit, so a warp of A and the warp of B on its scheduler take turns at
+        // the exponentials and work on their scores meanwhile.
+        if constexpr (kTurns)
+          if (nx == 2 && (x == 1 || j > 0)) {
+            ok = warp_wait_uniform(exp_turn(x, warp & 3), (uint32_t)(x == 1 ? j : j - 1) & 1u, abort_flag);
+            if (!ok) break;
           }
-          fence_async();
-        }
         const f32x2 sc2 = pack2(sc, sc), neg_m2 = pack2(bias - m_safe, bias - m_safe);
         f32x2 rs2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
@@ -462,13 +501,15 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
             pk[c >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
           }
           tmem_st16(t_s + 16u * h, pk);
-          if (h == kPosP / 64 - 1) {                 // half of P is there: its product may begin
+          if (kHalves && h == kPosP / 64 - 1) {                 // half of P is there: its product may begin
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(p_half(u));
           }
         }
+        if constexpr (kTurns)
+          if (nx == 2 && lane == 0) mbar_arrive(exp_turn(x ^ 1, warp & 3));
         float rs_lo, rs_hi;
         unpack2(add2(rs2[0], rs2[1]), rs_lo, rs_hi);
         l_run = l_run * corr + (rs_lo + rs_hi);
@@ -484,9 +525,9 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
     }
     if (!ok && lane == 0) *abort_flag = 1;
     // (a wait that gave up leaves the others of the CTA to theirs: all softmax warps come here)
-    asm volatile("barrier.sync.aligned 1, 256;" ::: "memory");
-    if (!*abort_flag && (x == 0 || two)) {
-      const bool odd = edges && *odd_flag, none = l_run == 0.f;
+    asm volatile("barrier.sync.aligned 1, %0;" ::"n"(128 * C::kGroups) : "memory");
+    if (!*abort_flag && x < nx) {
+      const bool odd = *odd_flag, none = l_run == 0.f;
       const float inv = none ? 0.f : 1.f / l_run;
       const long long at = ((long long)cta.split * a.kv.rows + tok) * a.Hq + head;
       // where this thread's row goes (elements of the output or of the parts), -1: nowhere
@@ -547,32 +588,33 @@ __global__ void __launch_bounds__(kThreadsP, 1) paged_attn_umma_kernel(const __g
 }
 
 // The softmax warpgroups take more registers a thread and leave the other fewer: the launch has to have them all (else they would wait).
-template <int HD, int FORM, bool ONE>
+template <int HD, int FORM, int NX>
 bool registers_add_up() {
+  using C = UCfg<HD, NX>;
   cudaFuncAttributes at{};
-  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM, ONE>) == cudaSuccess && at.numRegs * kThreadsP >= kRegsRest * 128 + kRegsSoftmax * 256;
+  return cudaFuncGetAttributes(&at, paged_attn_umma_kernel<HD, FORM, NX>) == cudaSuccess && at.numRegs * C::kThreads >= C::kRegsRest * 128 + C::kRegsSoftmax * 128 * C::kGroups;
 }
 
-template <int HD, int FORM, bool ONE>
+template <int HD, int FORM, int NX>
 bool launch(const PagedAttnArgs& a, const CUtensorMap& tk, const CUtensorMap& tv, int box_rows, cudaStream_t st) {
-  using C = UCfg<HD>;
-  static const bool fits = registers_add_up<HD, FORM, ONE>();
+  using C = UCfg<HD, NX>;
+  static const bool fits = registers_add_up<HD, FORM, NX>();
   if (!fits) return false;
   static PerDeviceOnce configured;
-  configured.run([] { cudaFuncSetAttribute(paged_attn_umma_kernel<HD, FORM, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes); });
-  const int row_tiles = (int)(((long long)a.kv.max_new * a.G + 255) / 256);
-  launch_pdl(paged_attn_umma_kernel<HD, FORM, ONE>, dim3((unsigned)((long long)a.kv.Hkv * row_tiles * a.splits * a.kv.batch)), dim3(kThreadsP), C::kSmemBytes, st, tk, tv, a,
+  configured.run([] { cudaFuncSetAttribute(paged_attn_umma_kernel<HD, FORM, NX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes); });
+  const int row_tiles = (int)(((long long)a.kv.max_new * a.G + 128 * C::kGroups - 1) / (128 * C::kGroups));
+  launch_pdl(paged_attn_umma_kernel<HD, FORM, NX>, dim3((unsigned)((long long)a.kv.Hkv * row_tiles * a.splits * a.kv.batch)), dim3(C::kThreads), C::kSmemBytes, st, tk, tv, a,
              row_tiles, box_rows);
   return true;
 }
 
-template <int HD, bool ONE>
+template <int HD, int NX>
 bool launch_form(const PagedAttnArgs& a, int form, const CUtensorMap& tk, const CUtensorMap& tv, int box, cudaStream_t st) {
   switch (form) {
-    case 0: return launch<HD, 0, ONE>(a, tk, tv, box, st);
-    case kCap: return launch<HD, kCap, ONE>(a, tk, tv, box, st);
-    case kBias: return launch<HD, kBias, ONE>(a, tk, tv, box, st);
-    default: return launch<HD, kCap + kBias, ONE>(a, tk, tv, box, st);
+    case 0: return launch<HD, 0, NX>(a, tk, tv, box, st);
+    case kCap: return launch<HD, kCap, NX>(a, tk, tv, box, st);
+    case kBias: return launch<HD, kBias, NX>(a, tk, tv, box, st);
+    default: return launch<HD, kCap + kBias, NX>(a, tk, tv, box, st);
   }
 }
 
@@ -584,9 +626,12 @@ bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
   const int box = paged_box_rows(a.kv.page_size);
   if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
   const int form = (a.softcap > 0.f ? kCap : 0) + (a.slopes || !(a.scale > 0.f) ? kBias : 0);
-  const bool one = (long long)a.kv.max_new * a.G <= 128;
-  if (a.kv.hd == 64) return one ? launch_form<64, true>(a, form, tk, tv, box, st) : launch_form<64, false>(a, form, tk, tv, box, st);
-  return one ? launch_form<128, true>(a, form, tk, tv, box, st) : launch_form<128, false>(a, form, tk, tv, box, st);
+  const long long rows = (long long)a.kv.max_new * a.G;
+  if (a.kv.hd == 64) {
+    if (rows <= 128) return launch_form<64, 1>(a, form, tk, tv, box, st);
+    return rows > 256 && a.splits == 1 ? launch_form<64, 4>(a, form, tk, tv, box, st) : launch_form<64, 2>(a, form, tk, tv, box, st);
+  }
+  return rows <= 128 ? launch_form<128, 1>(a, form, tk, tv, box, st) : launch_form<128, 2>(a, form, tk, tv, box, st);
 }
 
 }  // namespace nz
