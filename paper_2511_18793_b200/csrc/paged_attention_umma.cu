@@ -167,7 +167,16 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
   auto k_at = [&](int t) { return t < lead ? t : 2 * t - lead + 1; };
   auto v_at = [&](int t) { return lead + 2 * t; };
 
-  if (threadIdx.x == 0) {
+  // The boxes of all tiles are numbered through; a lane has the page of one in 32 of them, looked up 32 boxes ahead.
+  const int nb = kPosP / box_rows;
+  auto look_up = [&](int box) {
+    box += lane;
+    const int j = box / nb;
+    return j < NT ? page_of(a.kv, b, tile_at(j) * kPosP + (box - j * nb) * box_rows, box_rows, u_lo, u_hi) : 0;
+  };
+  int first_pages[2] = {0, 0};
+  if (warp == 0) { first_pages[0] = look_up(0); first_pages[1] = look_up(32); }
+  if (threadIdx.x == 64) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int x = 0; x < 4; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); mbar_init(q_full(x), 4); }
     for (int i = 0; i < 8; ++i) mbar_init(exp_turn(i >> 2, i & 3), 1);
@@ -191,17 +200,8 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
     if (warp == 0) {
       // ------------------------------------------------------------------ copies: K_0, V_0, K_1, V_1, ... through one ring
       const uint32_t leader = elect_one();
-      const int nb = kPosP / box_rows;
-      // the boxes of all tiles are numbered through; a lane has the page of one in 32 of them, looked up 32 boxes ahead
-      auto look_up = [&](int box) {
-        box += lane;
-        const int j = box / nb;
-        return j < NT ? page_of(a.kv, b, tile_at(j) * kPosP + (box - j * nb) * box_rows, box_rows, u_lo, u_hi) : 0;
-      };
       // (of each of K and V: the pages of its present 32 boxes and of the next)
-      int page[2], next[2], last = -1;
-      page[0] = page[1] = look_up(0);
-      next[0] = next[1] = look_up(32);
+      int page[2] = {first_pages[0], first_pages[0]}, next[2] = {first_pages[1], first_pages[1]}, last = -1;
       auto bring = [&](int kv, int t, int i) {
         const int s = i % SR, first = t * nb;        // (nb divides 32)
         if (i >= SR && !warp_wait_uniform(empty_bar(s), (uint32_t)(i / SR - 1) & 1u, abort_flag)) return false;
@@ -350,18 +350,25 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegsSoftmax));
     // ------------------------------------------------------------------ softmax, one thread per row
-    // a thread brings its own query row into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist, while the first tiles are on their way
+    // a warp brings its query rows into shared memory (K-major, 128-byte swizzle), zeros for rows that do not exist, while the first tiles are on their way
     const int x = (warp >> 2) - 1;                    // row tile of a softmax thread
     const int row = (warp & 3) * 32 + lane;           // = the TMEM lane this thread may read
     const bool live = r0 + x * 128 + row < R;
     const int rr = live ? r0 + x * 128 + row : r0;
     const int tok = sq.row0 + rr / G, head = kvh * G + rr % G, pos = first_p + rr / G;
     const Visible vis = live ? visible(a, pos, sq.len) : Visible{0, 0};
-    const uint4* src = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + (long long)tok * a.q_stride + (long long)head * HD);
+    const long long src = live ? (long long)tok * a.q_stride + (long long)head * HD : -1;
+    constexpr int kPieces = HD / 8;                   // of 16 bytes; neighbouring lanes take those of one row (each its own row's: 32 cache lines a load, 5,700 cycles)
+    uint4 qv[kPieces];
 #pragma unroll
-    for (int c = 0; c < HD / 8; ++c) {
-      const uint4 v = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-      *reinterpret_cast<uint4*>(gen_base + x * C::kQBytes + (c >> 3) * (128 * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+    for (int i = 0; i < kPieces; ++i) {
+      const long long from = __shfl_sync(0xffffffffu, src, i * (32 / kPieces) + lane / kPieces);
+      qv[i] = from >= 0 ? *reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + from + lane % kPieces * 8) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int r = (warp & 3) * 32 + i * (32 / kPieces) + lane / kPieces, c = lane % kPieces;
+      *reinterpret_cast<uint4*>(gen_base + x * C::kQBytes + (c >> 3) * (128 * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = qv[i];
     }
     fence_async();
     __syncwarp();
@@ -532,7 +539,8 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
       const long long at = ((long long)cta.split * a.kv.rows + tok) * a.Hq + head;
       // where this thread's row goes (elements of the output or of the parts), -1: nowhere
       const long long mine = !live || (a.splits > 1 && none) ? -1 : a.splits > 1 ? at * HD : (long long)tok * a.out_stride + (long long)head * HD;
-      float4* turn = reinterpret_cast<float4*>(gen_base + x * C::kQBytes) + (warp & 3) * 256;
+      // Turned in shared memory, where Q_X was, so that neighbouring lanes have neighbouring pieces of a row (each its own row's: 2,800 cycles)
+      uint8_t* turn = gen_base + x * C::kQBytes + (warp & 3) * (32 * HD * 2);
 #pragma unroll 1
       for (int c = 0; c < HD / 32; ++c) {
         float ov[32];
@@ -554,22 +562,37 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
           }
           __syncwarp();
         }
-        // turned in shared memory, where Q_X was, so that neighbouring lanes have neighbouring pieces of a row (each its own row's: 2,800 cycles)
+        if (a.splits == 1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          turn[lane * 8 + (i ^ (lane & 7))] = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(ov[4 * i] * inv, ov[4 * i + 1] * inv, ov[4 * i + 2] * inv, ov[4 * i + 3] * inv);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 4 * i + (lane >> 3);         // row of the warp's 32
-          const float4 v = turn[r * 8 + ((lane & 7) ^ (r & 7))];
-          const long long to = __shfl_sync(0xffffffffu, mine, r);
-          if (to >= 0) {
-            if (a.splits > 1) *reinterpret_cast<float4*>(a.part_o + to + 32 * c + 4 * (lane & 7)) = v;
-            else *reinterpret_cast<uint2*>((__nv_bfloat16*)a.out + to + 32 * c + 4 * (lane & 7)) = pack_bf16x4(v.x, v.y, v.z, v.w);
+          for (int i = 0; i < 4; ++i) {
+            const uint2 lo = pack_bf16x4(ov[8 * i] * inv, ov[8 * i + 1] * inv, ov[8 * i + 2] * inv, ov[8 * i + 3] * inv);
+            const uint2 hi = pack_bf16x4(ov[8 * i + 4] * inv, ov[8 * i + 5] * inv, ov[8 * i + 6] * inv, ov[8 * i + 7] * inv);
+            *reinterpret_cast<uint4*>(turn + lane * (HD * 2) + (((4 * c + i) ^ (lane & 7)) << 4)) = none ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(lo.x, lo.y, hi.x, hi.y);
           }
+        } else {                                     // parts are in 32 bits, 32 columns at a time
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<float4*>(turn + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_float4(ov[4 * i] * inv, ov[4 * i + 1] * inv, ov[4 * i + 2] * inv, ov[4 * i + 3] * inv);
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);       // row of the warp's 32
+            const float4 v = *reinterpret_cast<const float4*>(turn + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+            const long long to = __shfl_sync(0xffffffffu, mine, r);
+            if (to >= 0) *reinterpret_cast<float4*>(a.part_o + to + 32 * c + 4 * (lane & 7)) = v;
+          }
+          __syncwarp();
         }
+      }
+      if (a.splits == 1) {
         __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int r = i * (32 / kPieces) + lane / kPieces, piece = lane % kPieces;
+          const uint4 v = *reinterpret_cast<const uint4*>(turn + r * (HD * 2) + ((piece ^ (r & 7)) << 4));
+          const long long to = __shfl_sync(0xffffffffu, mine, r);
+          if (to >= 0) *reinterpret_cast<uint4*>((__nv_bfloat16*)a.out + to + 8 * piece) = v;
+        }
       }
       if (live) {
         const float lse2 = none ? -INFINITY : m_ref + log2f(l_run);
