@@ -119,7 +119,6 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
   constexpr int SR = C::kSlots, NH = HD / 64, KS = HD / 16, kPosP = C::kPos;
   constexpr bool ONE = NX == 1;
   constexpr bool kHalves = NX < 4;      // P V begins when half of P is there
-  constexpr bool kTurns = NX == 2 && (FORM & kCap) != 0;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
@@ -131,12 +130,11 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
   auto o_full = [&](int x) { return bar_base + 8u * (2 * SR + 8 + x); };      // (ONE: O_A holds tile j, x = j % 2)
   auto p_half = [&](int x) { return bar_base + 8u * (2 * SR + 12 + x); };      // its first 64 positions are
   auto q_full = [&](int x) { return bar_base + 8u * (2 * SR + 16 + x); };      // Q_X is in shared memory
-  auto exp_turn = [&](int x, int w) { return bar_base + 8u * (2 * SR + 20 + 4 * x + w); };      // warp w of rows x may go through its exponentials
-  const uint32_t edge_bar = bar_base + 8u * (2 * SR + 28), clean_bar = edge_bar + 8u;      // the next V tile on the edge is in its slot; what no row sees is out of it
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 30));
+  const uint32_t edge_bar = bar_base + 8u * (2 * SR + 20), clean_bar = edge_bar + 8u;      // the next V tile on the edge is in its slot; what no row sees is out of it
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + (bar_base - base) + 8 * (2 * SR + 22));
   volatile uint32_t* abort_flag = tmem_slot + 1;
   volatile uint32_t* odd_flag = tmem_slot + 2;      // a value that is not finite was taken out of a tile
-  static_assert(8 * (2 * SR + 30) + 12 <= C::kBarBytes, "barrier area");
+  static_assert(8 * (2 * SR + 22) + 12 <= C::kBarBytes, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   pdl_wait();
@@ -179,7 +177,6 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
   if (threadIdx.x == 64) {
     for (int s = 0; s < SR; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int x = 0; x < 4; ++x) { mbar_init(s_full(x), 1); mbar_init(p_full(x), 4); mbar_init(o_full(x), 1); mbar_init(p_half(x), 4); mbar_init(q_full(x), 4); }
-    for (int i = 0; i < 8; ++i) mbar_init(exp_turn(i >> 2, i & 3), 1);
     mbar_init(edge_bar, 1); mbar_init(clean_bar, 2);
     *abort_flag = 0; *odd_flag = 0;
     mbar_fence_init();
@@ -436,10 +433,10 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
         float bias = 0.f;                            // of the whole row: its scores are off by it until the exponential
         if constexpr ((FORM & kBias) != 0) {
           const float rel = (float)(pos - p0);
-          if (a.causal || p0 + kPosP - 1 <= pos_min) {
-            bias = -slope * rel;
+          if (p0 + kPosP - 1 <= pos_min) {           // counted from the tile's last position, so that no product is larger than the position's own distance makes it
+            bias = -slope * (rel - (float)(kPosP - 1));
 #pragma unroll
-            for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(slope, (float)c, sv[c]);
+            for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(slope, (float)(c - (kPosP - 1)), sv[c]);
           } else {
 #pragma unroll
             for (int c = 0; c < kPosP; ++c) sv[c] = fmaf(-slope, fabsf(rel - (float)c), sv[c]);
@@ -485,13 +482,6 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
             tmem_st16(t_o + 32u * c + 16u, ov + 16);
           }
         }
-        // Capped scores take as many instructions as the exponentials take cycles of their unit, so a warp of A and the warp of B on its scheduler take turns at
-        // the exponentials and work on their scores meanwhile.
-        if constexpr (kTurns)
-          if (nx == 2 && (x == 1 || j > 0)) {
-            ok = warp_wait_uniform(exp_turn(x, warp & 3), (uint32_t)(x == 1 ? j : j - 1) & 1u, abort_flag);
-            if (!ok) break;
-          }
         const f32x2 sc2 = pack2(sc, sc), neg_m2 = pack2(bias - m_safe, bias - m_safe);
         f32x2 rs2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
@@ -515,8 +505,6 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
             if (lane == 0) mbar_arrive(p_half(u));
           }
         }
-        if constexpr (kTurns)
-          if (nx == 2 && lane == 0) mbar_arrive(exp_turn(x ^ 1, warp & 3));
         float rs_lo, rs_hi;
         unpack2(add2(rs2[0], rs2[1]), rs_lo, rs_hi);
         l_run = l_run * corr + (rs_lo + rs_hi);
