@@ -1347,7 +1347,7 @@ nezha_status nezha_quantize_rows(nezha_ctx* c, const void* x, int64_t x_stride, 
   if (!x || !q || !scale || M < 0 || K < 1 || x_stride < K) return fail(c, NEZHA_ERR_ARG, "nezha_quantize_rows: bad argument");
   if (const nezha_status s = check_device(c, "nezha_quantize_rows")) return s;
   if (!M) return NEZHA_OK;
-  launch_quantize_rows(x, x_stride, M, K, q, scale, c->bf16, c->st);
+  launch_quantize_rows(x, x_stride, M, K, q, scale, c->bf16, c->es.status, c->st);
   NZ_CUDA(c, cudaGetLastError());
   return NEZHA_OK;
 }

@@ -89,7 +89,7 @@ void launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, b
 // --------------------------------------------------------------------------------------------------
 // 8-bit projections
 // --------------------------------------------------------------------------------------------------
-void launch_quantize_rows(const void* x, long long x_stride, int M, int K, int8_t* q, float* scale, bool bf16, cudaStream_t st);
+void launch_quantize_rows(const void* x, long long x_stride, int M, int K, int8_t* q, float* scale, bool bf16, int* status, cudaStream_t st);
 
 struct GemmI8Args {
   const int8_t *A, *W; const float *a_scale, *w_scale, *bias;
