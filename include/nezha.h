@@ -296,7 +296,8 @@ typedef struct {
   const int32_t* kv_len;         /* device [batch] positions of each sequence, its new rows among them         */
   int32_t rows;                  /* rows of the call's matrices                                                */
   int32_t max_new, max_kv;       /* the most new rows and positions that a sequence may have; max_kv at most   */
-                                 /* max_pages * page_size.  They size the launch: tight bounds are faster       */
+                                 /* max_pages * page_size (attention: and 2^31 - 4096).  They size the launch:   */
+                                 /* tight bounds are faster                                                     */
 } nezha_paged_kv;
 
 /* Rotary positions: angle of pair i (of rot_dim / 2) at position p = p * f_i, f_i = theta^(-2 i / rot_dim) before scaling. */

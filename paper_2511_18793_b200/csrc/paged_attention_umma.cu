@@ -1,17 +1,22 @@
 // Attention over a paged cache on the Blackwell tensor path (tcgen05 + TMEM, bf16, heads of 64 and 128): calls of many query rows, which are bound by
 // the two products and the exponentials between them.
 //
-// A CTA has one (sequence, KV head), 256 query rows as two tiles A and B of 128 (tokens times the heads of the group), and a share of the context in
-// tiles of 128 positions.  Warp 0 brings K and V tiles into one ring by TMA (a box of 64 columns per page or piece of a page), warp 1 issues the products, warps
-// 4 to 7 and 8 to 11 are the softmax of A and of B, one thread per row (a TMEM lane is a row).  TMEM: S_A, S_B (128 columns each), O_A, O_B.
+// A CTA has one (sequence, KV head), up to NX tiles of 128 query rows (tokens times the heads of the group; below A, B, ...), and a share of the context in tiles
+// of 128 positions (NX = 4: 64).  Warp 0 brings K and V tiles into one ring by TMA (a box of 64 columns per page or piece of a page), warp 1 issues the
+// products, warps 2 and 3 look after V tiles on the edge of what the rows see, and from warp 4 each row tile has a warpgroup for its softmax, one thread per
+// row (a TMEM lane is a row).  TMEM: S of each row tile, then O of each.
 //   S_X = Q_X K^T, then the row's scores through registers: running reference maximum (raised only when the true one has grown by more
 //   than 8 in log2, when O is rescaled in TMEM), base-2 exponentials, P as bf16 over the columns that its scores came from;
 //   O_X += P V with P read from TMEM; S_X of the next tile is issued right behind it.
-// While one tile's rows go through softmax, the tensor core runs the other tile's products: P_A V, S_A', P_B V, S_B', ...
-// ONE, of calls of at most 128 rows: rows A have both buffers of S, so S of the next tile is there before the softmax of this one ends (148 such CTAs, heads of
-// 128 over 16k positions: 379 us, the rate of the memory; 459 with one buffer).  With 256 rows a third buffer made A and B fall into step: 977 us for 919.
-// What a row does not see has no part in its sums (see paged_attention_tc.cu); a thread looks after one position of a tile on the edge.
-// Waits are bounded as everywhere.
+// While one tile's rows go through softmax, the tensor core runs the other tiles' products: P_A V, S_A', P_B V, S_B', ...  At 128 positions by 128 rows the
+// products of heads of 128 take as many cycles as the exponentials (1,024 a row tile), those of 64 half; what is left over is the chain of one softmax thread.
+//   NX = 1, calls of at most 128 rows: A has two buffers of S, so S of the next tile is there before the softmax of this one ends (148 such CTAs, heads of
+//     128 over 16k positions: 380 us, the rate of the memory; 459 with one buffer).
+//   NX = 2: 4,096 tokens of 32 heads of 128 behind 16k positions 1,055 us, 1,170 TFLOP/s, 71 % of the tensor cores' measured rate.  A third buffer of S,
+//     or a second issuing warp, made A and B fall into step, where they want the same unit at the same time (heads of 64: 977 and 1,056 us for 919).
+//   NX = 4, heads of 64 (four tiles of heads of 128 do not fit in TMEM): four warps per scheduler hide one another's latencies.  The same call with heads of 64
+//     859 us (917 with NX = 2), a ragged batch of 32 with caps, biases and a window 280 (about 350).
+// What a row does not see has no part in its sums (see paged_attention_tc.cu).  Waits are bounded as everywhere.
 #include <math.h>
 #include <stdlib.h>
 
@@ -19,6 +24,8 @@
 #include "paged_attention.cuh"
 
 namespace nz {
+
+int sm_count();
 
 namespace {
 
@@ -322,7 +329,11 @@ __global__ void __launch_bounds__(UCfg<HD, NX>::kThreads, 1) paged_attn_umma_ker
         if (!on_edge(tile_at(j))) continue;
         const int i = v_at(j), s = i % SR;
         // (full_bar alone would not do: it may be phases behind or ahead of a warp that passes over the tiles between)
-        ok = warp_wait_uniform(edge_bar, edges & 1u, abort_flag) && warp_wait_uniform(full_bar(s), (uint32_t)(i / SR) & 1u, abort_flag);
+        // (the issuing warp may be all tiles away from the edge, each of which it waits for in bounds: so many times the bound)
+        int tries = 0;
+        do ok = warp_wait_uniform(edge_bar, edges & 1u, abort_flag);
+        while (!ok && ++tries <= NT && !__any_sync(0xffffffffu, *abort_flag));
+        ok = ok && warp_wait_uniform(full_bar(s), (uint32_t)(i / SR) & 1u, abort_flag);
         if (!ok) break;
         ++edges;
         for (int row = threadIdx.x - 64; row < kPosP; row += 64) {
@@ -638,9 +649,11 @@ bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
   if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
   const int form = (a.softcap > 0.f ? kCap : 0) + (a.slopes || !(a.scale > 0.f) ? kBias : 0);
   const long long rows = (long long)a.kv.max_new * a.G;
+  // (512 rows a CTA only where 256 would be more CTAs than SMs: with fewer, halves on two SMs are done sooner)
+  const bool many = rows > 256 && a.splits == 1 && (long long)a.kv.Hkv * a.kv.batch * ((rows + 255) / 256) > sm_count();
   if (a.kv.hd == 64) {
     if (rows <= 128) return launch_form<64, 1>(a, form, tk, tv, box, st);
-    return rows > 256 && a.splits == 1 ? launch_form<64, 4>(a, form, tk, tv, box, st) : launch_form<64, 2>(a, form, tk, tv, box, st);
+    return many ? launch_form<64, 4>(a, form, tk, tv, box, st) : launch_form<64, 2>(a, form, tk, tv, box, st);
   }
   return rows <= 128 ? launch_form<128, 1>(a, form, tk, tv, box, st) : launch_form<128, 2>(a, form, tk, tv, box, st);
 }

@@ -51,6 +51,26 @@ def test_interior_tiles_between_edges(hd, hq, hkv, new, form):
     check(p, form, rows=sorted({0, 1, new // 2, new - 2, new - 1, new, new + min(new, 40) - 1}))
 
 
+@pytest.mark.parametrize("form", [dict(), dict(causal=False), dict(window=500), dict(window=700, softcap=30.0), dict(softcap=4.0, slopes=True),
+                                  dict(window=333, slopes=True), dict(window=600, softcap=60.0, slopes=True)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_more_tiles_of_rows_than_multiprocessors(hd, form):
+    """Up to 516 rows of 64 pairs of a sequence and a KV head, ragged; what nobody sees is NaN."""
+    form = dict(form)
+    if form.get("slopes"):
+        form["slopes"] = torch.tensor([2.0 ** -(1 + h) for h in range(8)])
+    news = [129, 65, 64, 33, 0, 1] + [129, 100] * 13
+    lens = [1400, 1001, 700, 40, 90, 600] + [140, 100] * 13
+    p = Paged("bf16", news, lens, 8, 2, hd, 16, tail_rows=1)
+    window = form.get("window", 0)
+    if window:
+        for page in range((lens[0] - news[0] - window + 1) // 16):
+            p.k_pool[int(p.table[0, page])] = float("nan")
+            p.v_pool[int(p.table[0, page])] = float("inf")
+        torch.cuda.synchronize()
+    check(p, form, rows=sorted({0, 31, 32, 64, 96, 127, 128, 129, 193, 194, 200, 257, 290, 291, 292, 420, p.starts[-1] - 1}))
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("new", [1, 4, 14, 30, 60, 130])
 @pytest.mark.parametrize("form", [dict(softcap=200.0), dict(softcap=20.0), dict(softcap=1.5), dict(softcap=5.0, scale=-0.2), dict(scale=-0.125),
@@ -84,3 +104,21 @@ def test_pools_with_room_between(new):
     p.k_pool, p.v_pool = k, v
     torch.cuda.synchronize()
     check(p, rows=sorted({0, new // 2, new - 1}))
+
+
+def test_positions_end_below_two_to_the_31():
+    """A table that repeats one large page describes that many positions; a call that names them all is refused, one of few is served."""
+    from paged_helpers import engine
+    from paper_2511_18793_b200 import binding
+    eng = engine("fp32")
+    pool = torch.zeros(1, 1, 2 ** 20, 16, device="cuda")
+    table = torch.zeros(1, 2048, dtype=torch.int32, device="cuda")
+    start, length = torch.tensor([0, 1], dtype=torch.int32).cuda(), torch.tensor([3], dtype=torch.int32).cuda()
+    q = torch.ones(1, 1, 16, device="cuda")
+    torch.cuda.synchronize()
+    with pytest.raises(binding.NezhaError) as e:
+        eng.paged_attention(binding.PagedKV(pool, pool, table, start, length, 1, 2 ** 31 - 4095), q)
+    assert e.value.status == 1
+    out = eng.paged_attention(binding.PagedKV(pool, pool, table, start, length, 1, 2 ** 20), q)
+    eng.sync()
+    assert bool((out == 0).all())
