@@ -335,6 +335,7 @@ nezha_status nezha_kv_append(nezha_ctx* ctx, const nezha_paged_kv* kv, const voi
 
 /* What a row at position p sees of position t, and how:
  *   score = scale * q.k;  softcap > 0: score = softcap * tanh(score / softcap);  slopes: score -= slopes[head] * |p - t|
+ *   (softcap from 1e-6 |scale| to 1e30, with |scale| up to 1e12)
  *   causal 1: t <= p.  window > 0 (causal only): also t > p - window.  causal 0: every position of the sequence.
  * (p = kv_len - new rows + index of the row; it may be negative: with causal 1 such a row sees nothing.) */
 typedef struct {
@@ -366,7 +367,7 @@ nezha_status nezha_paged_attention(nezha_ctx* ctx, const nezha_paged_kv* kv, con
 /* Rows to 8 bits: scale[m] = max|x[m, :]| / 127 (rounded once), q[m, k] = 127 x[m, k] / max|x[m, :]|, the exact quotient rounded
  * to the nearest, halves to even.  A row of zeros: scale 0, q 0.  A row with an infinity or a NaN: scale NaN, q 0.
  *   x  device, the context's storage type, row m at x + m * x_stride (elements)      q  device int8 [M, K]      scale  device float [M]
- * For activations (M tokens) and, once, for weights (M output channels).  Asynchronous. */
+ * q and scale must not overlap x.  For activations (M tokens) and, once, for weights (M output channels).  Asynchronous. */
 nezha_status nezha_quantize_rows(nezha_ctx* ctx, const void* x, int64_t x_stride, int32_t M, int32_t K, int8_t* q, float* scale);
 
 /* C[M, N] (op)= (sum_k A[m, k] W[n, k]) * a_scale[m] * w_scale[n] + bias[n]:  A int8 [M, K], W int8 [N, K], row-major and dense, -128 allowed.

@@ -122,3 +122,13 @@ def test_positions_end_below_two_to_the_31():
     out = eng.paged_attention(binding.PagedKV(pool, pool, table, start, length, 1, 2 ** 20), q)
     eng.sync()
     assert bool((out == 0).all())
+
+
+def test_caps_out_of_range_are_refused_and_those_at_its_ends_served():
+    from test_gpu_paged_attention import bad_call
+    p = Paged("bf16", [40], [70], 4, 1, 64, 16)
+    for kw in (dict(softcap=1e-30), dict(softcap=1e-8, scale=0.125), dict(softcap=2e30), dict(softcap=1.0, scale=2e12), dict(softcap=1e-7, scale=-0.125)):
+        bad_call(p, 1, **kw)
+    p.q[::2] = 0                                         # rows whose scores are all zero
+    check(p, dict(softcap=1.25e-7, scale=0.125))
+    check(p, dict(softcap=1e30, scale=0.125))
