@@ -232,17 +232,23 @@ class PagedKV:
         n_pages, heads, page_size, hd = k_pool.shape
         self._heads, self._hd, self._dtype = heads, hd, k_pool.dtype
         self._need: Dict[tuple, int] = {}          # workspace bytes by the sizes of a call
-        self.max_new, self.max_kv = max_new, max_pages * page_size if max_kv is None else max_kv
+        self.max_new, self.max_kv = max_new, min(max_pages * page_size, 2 ** 31 - 4096) if max_kv is None else max_kv
+        assert -2 ** 31 <= self.max_kv < 2 ** 31
         st = k_pool.stride()
-        self._s = NezhaPagedKV(k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
-                               max(page_table.stride(0), max_pages), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr(), 0, 0, self.max_kv)
-        self._ref = C.byref(self._s)
+        self._fields = (k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
+                               max(page_table.stride(0), max_pages), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr())
+        self._forms: Dict[tuple, object] = {}      # the C structs of attention's forms without slopes
+        self._refs: Dict[int, object] = {}         # the C struct by the rows of a call; never written again, so calls from several threads may share it
 
     def _for(self, rows: int):
         """The C struct for a call of `rows` rows."""
-        self._s.rows = rows
-        self._s.max_new = rows if self.max_new is None or self.max_new > rows else self.max_new
-        return self._ref
+        ref = self._refs.get(rows)
+        if ref is None:
+            if len(self._refs) > 64:
+                self._refs.clear()
+            max_new = rows if self.max_new is None or self.max_new > rows else self.max_new
+            ref = self._refs[rows] = C.byref(NezhaPagedKV(*self._fields, rows, max_new, self.max_kv))
+        return ref
 
 
 class Engine:
@@ -508,7 +514,13 @@ class Engine:
             assert slopes.dtype == torch.float32 and slopes.numel() == heads
             sl = _ptr(slopes)
         assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (rows, heads))
-        form = C.byref(NezhaAttnForm(1 if causal else 0, window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl))
+        form = kv._forms.get((causal, window, scale, softcap)) if sl is None else None
+        if form is None:
+            form = C.byref(NezhaAttnForm(1 if causal else 0, window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl))
+            if sl is None:
+                if len(kv._forms) > 64:
+                    kv._forms.clear()
+                kv._forms[causal, window, scale, softcap] = form
         ref = kv._for(rows)
         key = (rows, heads, kv.max_new, kv.max_kv, causal, window)
         need = kv._need.get(key)

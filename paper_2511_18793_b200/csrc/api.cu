@@ -1237,7 +1237,7 @@ const char* rope_fault(const nezha_rope* r) {
 const char* attn_fault(const nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq, const nezha_attn_form* f) {
   if (const char* why = paged_fault(c, kv)) return why;
   if (!f) return "null form";
-  if (kv->max_kv > INT32_MAX - 4096) return "max_kv above 2^31 - 4096";      // (the end of the last tile is a position too)
+  if (kv->max_kv > INT32_MAX - 4095) return "max_kv above 2^31 - 4096";      // (the end of the last tile is a position too)
   if (Hq < 1 || Hq % kv->n_kv_heads || Hq / kv->n_kv_heads > 64) return "n_q_heads must be a multiple of n_kv_heads, at most 64 times it";
   if (f->causal != 0 && f->causal != 1) return "causal must be 0 or 1";
   if (f->window < 0 || (f->window > 0 && !f->causal)) return "a window must be positive, and causal";

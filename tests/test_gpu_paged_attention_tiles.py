@@ -132,3 +132,55 @@ def test_caps_out_of_range_are_refused_and_those_at_its_ends_served():
     p.q[::2] = 0                                         # rows whose scores are all zero
     check(p, dict(softcap=1.25e-7, scale=0.125))
     check(p, dict(softcap=1e30, scale=0.125))
+
+
+def test_threads_share_a_description():
+    """Calls of different numbers of rows and forms through one PagedKV, from two threads with an engine each."""
+    import threading
+    from paged_helpers import engine, reference
+    p = Paged("bf16", [9], [200], 4, 2, 64, 16)
+    few = Paged("bf16", [9], [200], 4, 2, 64, 16)
+    few.q = few.q[:, [1, 0, 3, 2]].contiguous()
+    few.row_start, few.kv_len, few.d_table, few.k_pool, few.v_pool = p.row_start, p.kv_len, p.d_table, p.k_pool, p.v_pool
+    kv = p.kv()
+    wants = [reference(p), reference(few, window=30)]
+    results, errors = [[], []], []
+    engines = [engine("bf16", stream=torch.cuda.Stream()) for _ in range(2)]
+
+    def work(i, q, form):
+        try:
+            eng = engines[i]
+            for n in range(40):
+                rows = q if n % 2 else torch.cat([q, q])          # (rows behind the last sequence are left alone)
+                results[i].append(eng.paged_attention(kv, rows, **form)[:9])
+            eng.sync()
+        except Exception as e:                                    # noqa: BLE001
+            errors.append(e)
+
+    qs = [p.q.cuda(), few.q.cuda()]
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=(i, qs[i], f)) for i, f in enumerate((dict(), dict(window=30)))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    torch.cuda.synchronize()
+    for got, (want, _, tol) in zip(results, wants):
+        for out in got:
+            assert bool(((out.double().cpu() - want).abs() <= tol).all())
+
+
+def test_a_table_of_more_positions_than_an_integer_counts():
+    from paged_helpers import engine
+    from paper_2511_18793_b200 import binding
+    eng = engine("fp32")
+    pool = torch.zeros(1, 1, 2 ** 20, 16, device="cuda")
+    table = torch.zeros(1, 4096, dtype=torch.int32, device="cuda")
+    start, length = torch.tensor([0, 1], dtype=torch.int32).cuda(), torch.tensor([3], dtype=torch.int32).cuda()
+    torch.cuda.synchronize()
+    kv = binding.PagedKV(pool, pool, table, start, length, 1)
+    assert kv.max_kv == 2 ** 31 - 4096
+    out = eng.paged_attention(kv, torch.ones(1, 1, 16, device="cuda"))
+    eng.sync()
+    assert bool((out == 0).all())
