@@ -7,6 +7,8 @@
 // S = Q K^T and O += P V in registers with a running maximum and sum; the KW groups take every KW-th tile and are merged at the end.
 // One token per sequence: RW = 1, KW = 2, 64 KB of ring, three CTAs per SM -- a warp's chain (scores, softmax, second product) takes about
 // as long as a tile's way from HBM, so six of them per SM keep the memory busy.
+// 64 tokens of 32 heads of 128 on 8, on up to 4,000 positions in pages of 16: 126 us, 5.5 TB/s of the copy's 6.5 (113 with a warm L2); one token on 32k
+// positions, heads of 64: 24 us with the join, of which the stream is 10.
 //
 // What a row does not see has no part in its sums: scores are replaced, not added to; values at positions outside what the CTA's rows see
 // are zeroed in the tile, and where only some of its rows see a position, values that are not finite are taken out of the tile and added to
