@@ -514,6 +514,7 @@ class Engine:
             assert slopes.dtype == torch.float32 and slopes.numel() == heads
             sl = _ptr(slopes)
         assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (rows, heads))
+        assert -2 ** 31 <= window < 2 ** 31
         form = kv._forms.get((causal, window, scale, softcap)) if sl is None else None
         if form is None:
             form = C.byref(NezhaAttnForm(1 if causal else 0, window, 1.0 / math.sqrt(hd) if scale is None else scale, softcap, sl))

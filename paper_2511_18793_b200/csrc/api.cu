@@ -1256,7 +1256,8 @@ PagedAttnArgs attn_args(nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq, cons
   PagedAttnArgs a{};
   a.kv = paged_view(c, kv);
   a.Hq = Hq; a.G = Hq / kv->n_kv_heads;
-  a.scale = f->scale; a.softcap = f->softcap; a.slopes = f->slopes; a.causal = f->causal; a.window = f->window;
+  a.scale = f->scale; a.softcap = f->softcap; a.slopes = f->slopes; a.causal = f->causal;
+  a.window = f->window >= kv->max_kv ? 0 : f->window;      // (one that no sequence is longer than; p - window stays in range)
   a.splits = 1;
   return a;
 }

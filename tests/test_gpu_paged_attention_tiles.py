@@ -184,3 +184,12 @@ def test_a_table_of_more_positions_than_an_integer_counts():
     out = eng.paged_attention(kv, torch.ones(1, 1, 16, device="cuda"))
     eng.sync()
     assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("dtype,hd", [("fp32", 16), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("new", [6, 40, 150])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 160, 159])
+def test_windows_longer_than_every_sequence(dtype, hd, new, window):
+    """Next to them: rows in front of their sequence's first position, which see nothing."""
+    p = Paged(dtype, [new, new], [new - 5, 160], 2, 1, hd, 16)
+    check(p, dict(window=window), rows=sorted({0, 4, 5, 6 % new, new - 1, new, 2 * new - 1}))
