@@ -43,9 +43,9 @@ __global__ void __launch_bounds__(32 * kWarpsS) paged_attn_simt_kernel(PagedAttn
   const int first_p = s.len - s.n;
   // what any row of the tile sees, cut to the split's share
   int lo = visible(a, first_p + r0 / a.G, s.len).lo, hi = visible(a, first_p + min(r0 + kRowsS - 1, R - 1) / a.G, s.len).hi;
-  if (a.splits > 1) {
-    lo = max(lo, split * a.split_tiles * kAttnTile);
-    hi = min(hi, (split + 1) * a.split_tiles * kAttnTile);
+  if (a.splits > 1) {      // (the last share of the longest contexts ends at 2^31)
+    lo = (int)max((long long)lo, (long long)split * a.split_tiles * kAttnTile);
+    hi = (int)min((long long)hi, (long long)(split + 1) * a.split_tiles * kAttnTile);
   }
   for (int i = threadIdx.x; i < kRowsS * HD; i += blockDim.x) {
     const int r = i / HD, d = i - r * HD, row = min(r0 + r, R - 1);
