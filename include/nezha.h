@@ -280,7 +280,7 @@ nezha_status nezha_gemm(nezha_ctx* ctx, const void* A, const void* W, void* C, i
  * + (t % page_size) * pos_stride, head_dim consecutive elements (v alike).  Both nestings of head and position are strides.
  * Sequence b's new rows are rows row_start[b] .. row_start[b + 1] - 1 of the call's matrices (none is legal) and its LAST
  * positions: the last of them is position kv_len[b] - 1.  Rows outside [row_start[0], row_start[batch]) are left alone.
- * Table entries behind the kv_len[b] positions are not read.
+ * Table entries behind the kv_len[b] positions are not read, nor those of pages that every row's window has left behind.
  * Pool pointers and strides must be multiples of 16 bytes; no two (page, head, position) may overlap.
  * Device contents are checked where they are used: a page outside [0, n_pages), a row range outside [0, rows] or not
  * ascending, kv_len outside [0, max_kv] or more than max_new rows read as zeros or leave the sequence's rows alone, and the next

@@ -66,14 +66,14 @@ __global__ void __launch_bounds__(32 * kWarpsS) paged_attn_simt_kernel(PagedAttn
   }
   for (int t0 = lo / kPosS * kPosS; t0 < hi; t0 += kPosS) {
     __syncthreads();
-    // a tile of positions; those behind `hi` and on bad pages are zeros
+    // a tile of positions; those outside [lo, hi), whose pages may have been given back, and those on bad pages are zeros
     constexpr int V = 16 / sizeof(T);
     for (int i = threadIdx.x; i < kPosS * (HD / V); i += blockDim.x) {
       const int j = i / (HD / V), c = (i - j * (HD / V)) * V, t = t0 + j;
       T kk[V], vv[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) kk[e] = vv[e] = from_f32<T>(0.f);
-      if (t < hi) {
+      if (t >= lo && t < hi) {
         const int page = a.kv.table[(long long)b * a.kv.table_stride + t / a.kv.page_size];
         if (page >= 0 && page < a.kv.n_pages) {
           const long long at = page * a.kv.page_stride + kvh * a.kv.head_stride + (long long)(t % a.kv.page_size) * a.kv.pos_stride + c;
