@@ -63,7 +63,7 @@ __device__ __forceinline__ Visible visible(const PagedAttnArgs& a, int p, int le
   Visible v{0, len};
   if (a.causal) {
     v.hi = min(len, p + 1);
-    if (a.window > 0) v.lo = max(0, p - a.window + 1);
+    if (a.window > 0) v.lo = max(0, max(p, 0) - a.window + 1);      // (p may be far below 0: p - window would wrap round)
   }
   if (v.hi < v.lo) v.hi = v.lo;
   return v;
