@@ -289,8 +289,8 @@ typedef struct {
   void *k, *v;                   /* device                                                                   */
   int64_t page_stride, head_stride, pos_stride;      /* elements                                              */
   int32_t n_pages, page_size, n_kv_heads, head_dim;  /* head_dim 16, 32, 64 or 128                             */
-  const int32_t* page_table;     /* device [batch, table_stride], of which max_pages entries per sequence      */
-  int64_t table_stride;
+  const int32_t* page_table;     /* device: max_pages entries per sequence, sequence b's from b * table_stride on */
+  int64_t table_stride;          /* rows may lie on one another (0: all sequences have the same pages)          */
   int32_t max_pages, batch;
   const int32_t* row_start;      /* device [batch + 1]                                                         */
   const int32_t* kv_len;         /* device [batch] positions of each sequence, its new rows among them         */

@@ -213,7 +213,7 @@ class PagedKV:
 
     k_pool, v_pool  [n_pages, n_kv_heads, page_size, head_dim], any strides with a dense last dimension: a pool that keeps positions
                     outside heads is passed as `pool.transpose(1, 2)`; the two have the same strides
-    page_table      int32 [batch, max_pages]
+    page_table      int32 [batch, max_pages], rows any distance apart: `history.expand(beams, -1)` is legal
     row_start       int32 [batch + 1], kv_len int32 [batch]
     max_new, max_kv the most new rows and positions of a sequence (default: all rows of the call, all positions of the table)
     """
@@ -236,7 +236,7 @@ class PagedKV:
         assert -2 ** 31 <= self.max_kv < 2 ** 31
         st = k_pool.stride()
         self._fields = (k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
-                               max(page_table.stride(0), max_pages), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr())
+                               page_table.stride(0), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr())
         self._forms: Dict[tuple, object] = {}      # the C structs of attention's forms without slopes
         self._refs: Dict[int, object] = {}         # the C struct by the rows of a call; never written again, so calls from several threads may share it
 

@@ -1195,7 +1195,7 @@ const char* paged_fault(const nezha_ctx* c, const nezha_paged_kv* p) {
   if (!p->k || !p->v || !p->page_table || !p->row_start || !p->kv_len) return "null pointer in the cache";
   if (p->head_dim != 16 && p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return "head_dim must be 16, 32, 64 or 128";
   if (p->n_pages < 1 || p->page_size < 1 || p->n_kv_heads < 1 || p->batch < 1 || p->max_pages < 1) return "a size of the cache is not positive";
-  if (p->table_stride < p->max_pages) return "table_stride below max_pages";
+  if (p->table_stride < 0) return "table_stride negative";
   if (p->rows < 0 || p->max_new < 0 || p->max_new > p->rows) return "rows, max_new out of range";
   if (p->max_kv < 0 || (int64_t)p->max_kv > (int64_t)p->max_pages * p->page_size) return "max_kv beyond max_pages * page_size";
   if (((uintptr_t)p->k & 15) || ((uintptr_t)p->v & 15)) return "pool not aligned to 16 bytes";
