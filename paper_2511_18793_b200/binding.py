@@ -204,7 +204,7 @@ class RopeTable:
     """What Engine.rope_table returns: the cosines and sines of positions 0 .. n - 1, float32 [n, rot_dim]."""
 
     def __init__(self, rope: Rope, table: torch.Tensor):
-        self.rope, self.table = rope, table
+        self.rope, self.table, self._dev = rope, table, table.get_device()
         self._ref = C.byref(rope.struct())
 
 
@@ -230,7 +230,7 @@ class PagedKV:
             assert t.device == k_pool.device and t.is_cuda
         self.k_pool, self.v_pool, self.page_table, self.row_start, self.kv_len = k_pool, v_pool, page_table, row_start, kv_len
         n_pages, heads, page_size, hd = k_pool.shape
-        self._heads, self._hd, self._dtype = heads, hd, k_pool.dtype
+        self._heads, self._hd, self._dtype, self._dev = heads, hd, k_pool.dtype, k_pool.get_device()
         self._need: Dict[tuple, int] = {}          # workspace bytes by the sizes of a call
         self.max_new, self.max_kv = max_new, min(max_pages * page_size, 2 ** 31 - 4096) if max_kv is None else max_kv
         assert -2 ** 31 <= self.max_kv < 2 ** 31
@@ -463,6 +463,13 @@ class Engine:
         with torch.cuda.stream(torch.cuda.default_stream(self.arena.device) if self.stream is None else self.stream):
             return torch.empty(shape, dtype=dtype, device=self.arena.device)
 
+    def _here(self, t: Optional[torch.Tensor]) -> Optional[int]:
+        """The address of a dense tensor of the engine's GPU."""
+        if t is None:
+            return None
+        assert t.get_device() == self._dev and t.is_contiguous()
+        return t.data_ptr()
+
     def _rows(self, t: torch.Tensor, heads: int, hd: int, rows: int) -> int:
         """Row stride of [rows, heads, hd] whose heads lie side by side."""
         st = t.stride()
@@ -480,7 +487,7 @@ class Engine:
         """k, v [rows, n_kv_heads, head_dim] (and q [rows, n_q_heads, head_dim]) of the new rows, e.g. slices of a fused QKV product.
         Returns the rotated q (q_out, a new tensor if not given; q itself is legal)."""
         heads, hd, rows = kv._heads, kv._hd, k.shape[0]
-        assert kv._dtype is self._dtype
+        assert kv._dtype is self._dtype and kv._dev == self._dev
         ks, vs = self._rows(k, heads, hd, rows), self._rows(v, heads, hd, rows)
         qp = op = None
         qs = os_ = hq = 0
@@ -490,13 +497,14 @@ class Engine:
             if q_out is None:
                 q_out = self._new((rows, hq, hd), q.dtype)
             os_, op = self._rows(q_out, hq, hd, rows), q_out.data_ptr()
-        assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == rows)
+        assert positions is None or (positions.dtype == torch.int32 and positions.numel() == rows)
         ref = tab = None
         n_table = 0
         if rope is not None:
+            assert rope._dev == self._dev
             ref, tab, n_table = rope._ref, rope.table.data_ptr(), rope.table.shape[0]
         st = lib.nezha_kv_append(self._h, kv._for(rows), qp, qs, hq, op, os_, k.data_ptr(), ks, v.data_ptr(), vs, ref, tab, n_table,
-                                 None if positions is None else _ptr(positions))
+                                 self._here(positions))
         if st:
             self._check(st)
         return q_out
@@ -507,12 +515,12 @@ class Engine:
         """Attention of the new rows q [rows, n_q_heads, head_dim] over their sequences' positions; scale: 1 / sqrt(head_dim) if not given;
         lse: float32 [rows, n_q_heads] to fill.  The workspace, where one is needed, is a new tensor of the call."""
         rows, heads, hd = q.shape
-        assert hd == kv._hd and kv._dtype is self._dtype
+        assert hd == kv._hd and kv._dtype is self._dtype and kv._dev == self._dev
         qs = self._rows(q, heads, hd, rows)
         sl = None
         if slopes is not None:
             assert slopes.dtype == torch.float32 and slopes.numel() == heads
-            sl = _ptr(slopes)
+            sl = self._here(slopes)
         assert lse is None or (lse.dtype == torch.float32 and tuple(lse.shape) == (rows, heads))
         assert -2 ** 31 <= window < 2 ** 31
         form = kv._forms.get((causal, window, scale, softcap)) if sl is None else None
@@ -537,7 +545,7 @@ class Engine:
             ws = self._new((need,), torch.uint8)
             wp = ws.data_ptr()
         st = lib.nezha_paged_attention(self._h, ref, q.data_ptr(), qs, heads, form, out.data_ptr(), self._rows(out, heads, hd, rows),
-                                       None if lse is None else _ptr(lse), wp, need)
+                                       self._here(lse), wp, need)
         if st:
             self._check(st)
         return out
@@ -552,7 +560,7 @@ class Engine:
         if scale is None:
             scale = self._new((M,), torch.float32)
         assert q.dtype is torch.int8 and q.shape == (M, K) and scale.dtype is torch.float32 and scale.numel() == M
-        st = lib.nezha_quantize_rows(self._h, x.data_ptr(), xs[0] if M > 1 else max(xs[0], K), M, K, _ptr(q), _ptr(scale))
+        st = lib.nezha_quantize_rows(self._h, x.data_ptr(), xs[0] if M > 1 else max(xs[0], K), M, K, self._here(q), self._here(scale))
         if st:
             self._check(st)
         return q, scale
@@ -565,7 +573,8 @@ class Engine:
         assert C_out.dtype is (self._dtype if epilogue == 0 else torch.float32)
         assert a_scale.dtype is torch.float32 and w_scale.dtype is torch.float32 and a_scale.numel() == M and w_scale.numel() == N
         assert bias is None or (bias.dtype is torch.float32 and bias.numel() == N)
-        st = lib.nezha_gemm_int8(self._h, _ptr(A), _ptr(a_scale), _ptr(W), _ptr(w_scale), _ptr(C_out), M, N, K, epilogue, _ptr(bias))
+        st = lib.nezha_gemm_int8(self._h, self._here(A), self._here(a_scale), self._here(W), self._here(w_scale), self._here(C_out), M, N, K, epilogue,
+                                 self._here(bias))
         if st:
             self._check(st)
         return C_out
