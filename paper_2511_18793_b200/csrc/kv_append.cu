@@ -82,9 +82,14 @@ __device__ __forceinline__ void look_over(const PagedView& kv) {
 // `lanes`-th head of q, then k, then v, so that it reads its cosines and sines once per row and its loads of up to kHeads heads are under way together.
 // (A thread per piece of one head, its table columns read again for each: 120 us for 16,008 rows of 32 + 8 + 8 heads of 128.)
 constexpr int kHeads = 6;
+// Threads of a block at most: they have to fit with kMaxRegs registers each (rows of more heads take further passes).  A few registers more cost a block per
+// SM: 16,008 rows of 32 + 8 + 8 heads of 128, half of a head rotated, 91 us with 96 and 114 with 98; pairs side by side 74 with 64 and 81 with 68.
+constexpr int kMaxThreads = 512;
+template <bool HALVES> constexpr int kMaxRegs = HALVES ? 96 : 64;
+static_assert(kMaxThreads * kMaxRegs<true> <= 65536, "registers of an SM");
 
 template <typename T, bool HALVES>
-__global__ void kv_append_kernel(AppendArgs a, int units, int turned, int lanes, int rows_per_block) {
+__global__ void __maxnreg__(kMaxRegs<HALVES>) kv_append_kernel(AppendArgs a, int units, int turned, int lanes, int rows_per_block) {
   constexpr int N = Vec<T>::N;
   __shared__ long long place[16];
   __shared__ int turn[16];
@@ -225,7 +230,7 @@ void launch_vec(const AppendArgs& a, cudaStream_t st) {
   const int turned = HALVES ? a.rot / 2 / N : a.rot / N, units = turned + (a.kv.hd - a.rot) / N, heads = a.Hq + 2 * a.kv.Hkv;
   // heads side by side: as few as keep all of a row's loads under way at once, and few rows' threads together a block of 128 or more
   int lanes = (heads + kHeads - 1) / kHeads;
-  if (lanes * units > 1024) lanes = 1024 / units;
+  if (lanes * units > kMaxThreads) lanes = kMaxThreads / units;
   int rows = 1;
   if (a.kv.rows > 8 * 148)
     while (rows < 16 && 2 * rows * lanes * units <= 256) rows *= 2;
