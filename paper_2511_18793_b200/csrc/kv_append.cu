@@ -9,6 +9,8 @@
 
 namespace nz {
 
+int sm_count();
+
 namespace {
 
 template <typename T> struct Vec;
@@ -232,7 +234,7 @@ void launch_vec(const AppendArgs& a, cudaStream_t st) {
   int lanes = (heads + kHeads - 1) / kHeads;
   if (lanes * units > kMaxThreads) lanes = kMaxThreads / units;
   int rows = 1;
-  if (a.kv.rows > 8 * 148)
+  if (a.kv.rows > 8 * sm_count())
     while (rows < 16 && 2 * rows * lanes * units <= 256) rows *= 2;
   const int threads = (rows * lanes * units + 31) / 32 * 32;
   launch_pdl(kv_append_kernel<T, HALVES>, dim3((a.kv.rows + rows - 1) / rows), dim3(threads), 0, st, a, units, turned, lanes, rows);
