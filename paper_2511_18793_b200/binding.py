@@ -532,12 +532,8 @@ class Engine:
                 kv._forms[causal, window, scale, softcap] = form
         ref = kv._for(rows)
         key = (rows, heads, kv.max_new, kv.max_kv, causal, window)
-        need = kv._need.get(key)
-        if need is None:
-            need = lib.nezha_paged_attention_workspace(self._h, ref, heads, form)
-            if len(kv._need) > 64:
-                kv._need.clear()
-            kv._need[key] = need
+        known = kv._need.get(key)
+        need = lib.nezha_paged_attention_workspace(self._h, ref, heads, form) if known is None else known
         if out is None:
             out = self._new((rows, heads, hd), q.dtype)
         ws = wp = None
@@ -548,6 +544,10 @@ class Engine:
                                        self._here(lse), wp, need)
         if st:
             self._check(st)
+        if known is None:                          # (kept of calls that were served: of a bad argument the size is 0 too)
+            if len(kv._need) > 64:
+                kv._need.clear()
+            kv._need[key] = need
         return out
 
     def quantize_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
