@@ -216,10 +216,18 @@ class PagedKV:
     page_table      int32 [batch, max_pages], rows any distance apart: `history.expand(beams, -1)` is legal
     row_start       int32 [batch + 1], kv_len int32 [batch]
     max_new, max_kv the most new rows and positions of a sequence (default: all rows of the call, all positions of the table)
+
+    They are attributes that may be set: the next call goes by what they say then.
     """
 
     def __init__(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor,
                  max_new: Optional[int] = None, max_kv: Optional[int] = None):
+        self._k_pool, self._v_pool, self._page_table, self._row_start, self._kv_len = k_pool, v_pool, page_table, row_start, kv_len
+        self._max_new, self._max_kv = max_new, max_kv
+        self._describe()
+
+    def _describe(self):
+        k_pool, v_pool, page_table, row_start, kv_len = self._k_pool, self._v_pool, self._page_table, self._row_start, self._kv_len
         assert k_pool.dim() == 4 and k_pool.shape == v_pool.shape and k_pool.dtype == v_pool.dtype
         assert k_pool.stride() == v_pool.stride() and k_pool.stride(3) == 1
         assert page_table.dim() == 2 and page_table.stride(1) == 1 and row_start.is_contiguous() and kv_len.is_contiguous()
@@ -228,27 +236,42 @@ class PagedKV:
         assert tuple(row_start.shape) == (batch + 1,) and tuple(kv_len.shape) == (batch,)
         for t in (v_pool, page_table, row_start, kv_len):
             assert t.device == k_pool.device and t.is_cuda
-        self.k_pool, self.v_pool, self.page_table, self.row_start, self.kv_len = k_pool, v_pool, page_table, row_start, kv_len
         n_pages, heads, page_size, hd = k_pool.shape
         self._heads, self._hd, self._dtype, self._dev = heads, hd, k_pool.dtype, k_pool.get_device()
-        self._need: Dict[tuple, int] = {}          # workspace bytes by the sizes of a call
-        self.max_new, self.max_kv = max_new, min(max_pages * page_size, 2 ** 31 - 4096) if max_kv is None else max_kv
-        assert -2 ** 31 <= self.max_kv < 2 ** 31
+        max_kv = self.max_kv
+        assert -2 ** 31 <= max_kv < 2 ** 31
         st = k_pool.stride()
-        self._fields = (k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
-                               page_table.stride(0), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr())
+        self._need: Dict[tuple, int] = {}          # workspace bytes by the sizes of a call
         self._forms: Dict[tuple, object] = {}      # the C structs of attention's forms without slopes
         self._refs: Dict[int, object] = {}         # the C struct by the rows of a call; never written again, so calls from several threads may share it
+        self._fields = (k_pool.data_ptr(), v_pool.data_ptr(), st[0], st[1], st[2], n_pages, page_size, heads, hd, page_table.data_ptr(),
+                        page_table.stride(0), max_pages, batch, row_start.data_ptr(), kv_len.data_ptr())
 
     def _for(self, rows: int):
         """The C struct for a call of `rows` rows."""
+        if self._fields is None:
+            self._describe()
         ref = self._refs.get(rows)
         if ref is None:
             if len(self._refs) > 64:
                 self._refs.clear()
-            max_new = rows if self.max_new is None or self.max_new > rows else self.max_new
+            max_new = rows if self._max_new is None or self._max_new > rows else self._max_new
             ref = self._refs[rows] = C.byref(NezhaPagedKV(*self._fields, rows, max_new, self.max_kv))
         return ref
+
+
+def _described(name: str):
+    """An attribute of a PagedKV that may be set: the next call describes the cache anew."""
+    def put(self, value):
+        setattr(self, "_" + name, value)
+        self._fields = None
+    return property(lambda self: getattr(self, "_" + name), put)
+
+
+for _name in ("k_pool", "v_pool", "page_table", "row_start", "kv_len", "max_new", "max_kv"):
+    setattr(PagedKV, _name, _described(_name))
+PagedKV.max_kv = PagedKV.max_kv.getter(
+    lambda self: min(self._page_table.shape[1] * self._k_pool.shape[2], 2 ** 31 - 4096) if self._max_kv is None else self._max_kv)
 
 
 class Engine:
@@ -486,7 +509,9 @@ class Engine:
                   positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """k, v [rows, n_kv_heads, head_dim] (and q [rows, n_q_heads, head_dim]) of the new rows, e.g. slices of a fused QKV product.
         Returns the rotated q (q_out, a new tensor if not given; q itself is legal)."""
-        heads, hd, rows = kv._heads, kv._hd, k.shape[0]
+        rows = k.shape[0]
+        described = kv._for(rows)
+        heads, hd = kv._heads, kv._hd
         assert kv._dtype is self._dtype and kv._dev == self._dev
         ks, vs = self._rows(k, heads, hd, rows), self._rows(v, heads, hd, rows)
         qp = op = None
@@ -503,7 +528,7 @@ class Engine:
         if rope is not None:
             assert rope._dev == self._dev
             ref, tab, n_table = rope._ref, rope.table.data_ptr(), rope.table.shape[0]
-        st = lib.nezha_kv_append(self._h, kv._for(rows), qp, qs, hq, op, os_, k.data_ptr(), ks, v.data_ptr(), vs, ref, tab, n_table,
+        st = lib.nezha_kv_append(self._h, described, qp, qs, hq, op, os_, k.data_ptr(), ks, v.data_ptr(), vs, ref, tab, n_table,
                                  self._here(positions))
         if st:
             self._check(st)
@@ -515,6 +540,7 @@ class Engine:
         """Attention of the new rows q [rows, n_q_heads, head_dim] over their sequences' positions; scale: 1 / sqrt(head_dim) if not given;
         lse: float32 [rows, n_q_heads] to fill.  The workspace, where one is needed, is a new tensor of the call."""
         rows, heads, hd = q.shape
+        described = kv._for(rows)
         assert hd == kv._hd and kv._dtype is self._dtype and kv._dev == self._dev
         qs = self._rows(q, heads, hd, rows)
         sl = None
@@ -530,17 +556,16 @@ class Engine:
                 if len(kv._forms) > 64:
                     kv._forms.clear()
                 kv._forms[causal, window, scale, softcap] = form
-        ref = kv._for(rows)
-        key = (rows, heads, kv.max_new, kv.max_kv, causal, window)
+        key = (rows, heads, causal, window)
         known = kv._need.get(key)
-        need = lib.nezha_paged_attention_workspace(self._h, ref, heads, form) if known is None else known
+        need = lib.nezha_paged_attention_workspace(self._h, described, heads, form) if known is None else known
         if out is None:
             out = self._new((rows, heads, hd), q.dtype)
         ws = wp = None
         if need:
             ws = self._new((need,), torch.uint8)
             wp = ws.data_ptr()
-        st = lib.nezha_paged_attention(self._h, ref, q.data_ptr(), qs, heads, form, out.data_ptr(), self._rows(out, heads, hd, rows),
+        st = lib.nezha_paged_attention(self._h, described, q.data_ptr(), qs, heads, form, out.data_ptr(), self._rows(out, heads, hd, rows),
                                        self._here(lse), wp, need)
         if st:
             self._check(st)

@@ -37,3 +37,19 @@ def test_the_stride_of_a_table_is_its_own():
     assert described(paged(on_gpu(torch.zeros(20, dtype=torch.int32)).as_strided((3, 4), (1, 1))), 1).table_stride == 1
     # of one sequence it does not matter
     assert described(paged(wide[:1, :4].expand(1, 4)), 1).table_stride >= 0
+
+
+def test_attributes_that_are_set():
+    kv = paged()
+    assert kv.max_kv == 4 * 16 and kv.max_new is None
+    first = described(kv, 5)
+    assert (first.max_kv, first.max_new, first.rows) == (64, 5, 5) and described(kv, 5) is first
+    kv.max_kv, kv.max_new = 40, 2
+    assert (described(kv, 5).max_kv, described(kv, 5).max_new) == (40, 2) and (first.max_kv, first.max_new) == (64, 5)
+    kv.max_kv = None
+    kv.page_table = on_gpu(torch.zeros(3, 7, dtype=torch.int32))
+    assert kv.max_kv == 7 * 16 == described(kv, 5).max_kv and described(kv, 5).max_pages == 7
+    kv.kv_len += 1                                   # the same tensor
+    assert described(kv, 5).kv_len == kv.kv_len.data_ptr()
+    lens = kv.kv_len = on_gpu(torch.ones(3, dtype=torch.int32))
+    assert described(kv, 5).kv_len == lens.data_ptr()
