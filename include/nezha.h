@@ -328,7 +328,7 @@ nezha_status nezha_rope_table(nezha_ctx* ctx, const nezha_rope* rope, float* tab
  *   positions device int32 [rows] or NULL: rotary position of each row where that is not its position in the sequence
  * All pointers and strides must be multiples of 16 bytes.  Rounded once, to the storage type.  Two rows of one call
  * must not share a place in the pool.  A row of which something is out of bounds is not written at all (NEZHA_ERR_PAGE).
- * Asynchronous. */
+ * Asynchronous; without rows nothing is done, and the matrices may be null. */
 nezha_status nezha_kv_append(nezha_ctx* ctx, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads,
                              void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                              const nezha_rope* rope, const float* table, int32_t n_table, const int32_t* positions);
@@ -355,7 +355,7 @@ size_t nezha_paged_attention_workspace(nezha_ctx* ctx, const nezha_paged_kv* kv,
  *              work is done.  Calls that can overlap need workspaces of their own.
  * A row that sees nothing gets zeros.  Positions that a row does not see have no part in its result, whatever they hold.
  * bf16: products of bf16 operands, sums, softmax statistics and the output's accumulator in 32 bits; the weights are rounded to bf16 for the
- * second product, the result once.  The same call on the same contents returns the same bits.  Asynchronous. */
+ * second product, the result once.  The same call on the same contents returns the same bits.  Asynchronous; without rows nothing is done. */
 nezha_status nezha_paged_attention(nezha_ctx* ctx, const nezha_paged_kv* kv, const void* q, int64_t q_stride, int32_t n_q_heads,
                                    const nezha_attn_form* form, void* out, int64_t out_stride, float* lse,
                                    void* workspace, size_t workspace_bytes);

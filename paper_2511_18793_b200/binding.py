@@ -598,6 +598,8 @@ class Engine:
         assert C_out.dtype is (self._dtype if epilogue == 0 else torch.float32)
         assert a_scale.dtype is torch.float32 and w_scale.dtype is torch.float32 and a_scale.numel() == M and w_scale.numel() == N
         assert bias is None or (bias.dtype is torch.float32 and bias.numel() == N)
+        if M == 0:                                 # (the C entry wants a row, as nezha_gemm does)
+            return C_out
         st = lib.nezha_gemm_int8(self._h, self._here(A), self._here(a_scale), self._here(W), self._here(w_scale), self._here(C_out), M, N, K, epilogue,
                                  self._here(bias))
         if st:

@@ -1267,8 +1267,8 @@ PagedAttnArgs attn_args(nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq, cons
 nezha_status nezha_rope_table(nezha_ctx* c, const nezha_rope* r, float* table, int32_t n_positions) {
   if (!c) return NEZHA_ERR_ARG;
   const char* why = rope_fault(r);
-  if (!why && (!table || ((uintptr_t)table & 15))) why = "table null or not aligned to 16 bytes";
   if (!why && n_positions < 0) why = "n_positions negative";
+  if (!why && n_positions && (!table || ((uintptr_t)table & 15))) why = "table null or not aligned to 16 bytes";
   if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_rope_table: ") + why);
   if (const nezha_status s = check_device(c, "nezha_rope_table")) return s;
   if (!n_positions) return NEZHA_OK;
@@ -1298,6 +1298,7 @@ nezha_status nezha_kv_append(nezha_ctx* c, const nezha_paged_kv* kv, const void*
                              const float* table, int32_t n_table, const int32_t* positions) {
   if (!c) return NEZHA_ERR_ARG;
   const char* why = paged_fault(c, kv);
+  if (!why && !kv->rows) return NEZHA_OK;              // (the matrices of a call without rows may be null)
   const int64_t kv_width = why ? 0 : (int64_t)kv->n_kv_heads * kv->head_dim;
   if (!why) why = rows_fault(c, k, k_stride, kv_width, "k");
   if (!why) why = rows_fault(c, v, v_stride, kv_width, "v");
@@ -1314,7 +1315,6 @@ nezha_status nezha_kv_append(nezha_ctx* c, const nezha_paged_kv* kv, const void*
   if (!why && (int64_t)((q ? n_q_heads : 0) + 2 * kv->n_kv_heads) * kv->head_dim > (1 << 24)) why = "too many heads";
   if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_kv_append: ") + why);
   if (const nezha_status s = check_device(c, "nezha_kv_append")) return s;
-  if (!kv->rows) return NEZHA_OK;
   AppendArgs a{paged_view(c, kv), q, q_stride, q ? n_q_heads : 0, q_out, q_out_stride, k, k_stride, v, v_stride,
                rope ? rope->rot_dim : 0, rope ? rope->interleaved : 0, table, rope ? n_table : 0, positions};
   launch_kv_append(a, c->bf16, c->st);
@@ -1331,11 +1331,11 @@ nezha_status nezha_paged_attention(nezha_ctx* c, const nezha_paged_kv* kv, const
                                    const nezha_attn_form* form, void* out, int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes) {
   if (!c) return NEZHA_ERR_ARG;
   const char* why = attn_fault(c, kv, n_q_heads, form);
+  if (!why && !kv->max_new) return NEZHA_OK;           // (the matrices of a call without rows may be null)
   if (!why) why = rows_fault(c, q, q_stride, (int64_t)n_q_heads * kv->head_dim, "q");
   if (!why) why = rows_fault(c, out, out_stride, (int64_t)n_q_heads * kv->head_dim, "out");
   if (why) return fail(c, NEZHA_ERR_ARG, std::string("nezha_paged_attention: ") + why);
   if (const nezha_status s = check_device(c, "nezha_paged_attention")) return s;
-  if (!kv->max_new) return NEZHA_OK;
   PagedAttnArgs a = attn_args(c, kv, n_q_heads, form);
   a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   const PagedAttnPlan plan = paged_attn_plan(a, c->bf16);
@@ -1349,9 +1349,9 @@ nezha_status nezha_paged_attention(nezha_ctx* c, const nezha_paged_kv* kv, const
 
 nezha_status nezha_quantize_rows(nezha_ctx* c, const void* x, int64_t x_stride, int32_t M, int32_t K, int8_t* q, float* scale) {
   if (!c) return NEZHA_ERR_ARG;
-  if (!x || !q || !scale || M < 0 || K < 1 || x_stride < K) return fail(c, NEZHA_ERR_ARG, "nezha_quantize_rows: bad argument");
-  if (const nezha_status s = check_device(c, "nezha_quantize_rows")) return s;
+  if (M < 0 || K < 1 || x_stride < K || (M && (!x || !q || !scale))) return fail(c, NEZHA_ERR_ARG, "nezha_quantize_rows: bad argument");
   if (!M) return NEZHA_OK;
+  if (const nezha_status s = check_device(c, "nezha_quantize_rows")) return s;
   launch_quantize_rows(x, x_stride, M, K, q, scale, c->bf16, c->es.status, c->st);
   NZ_CUDA(c, cudaGetLastError());
   return NEZHA_OK;
