@@ -335,7 +335,7 @@ nezha_status nezha_kv_append(nezha_ctx* ctx, const nezha_paged_kv* kv, const voi
 
 /* What a row at position p sees of position t, and how:
  *   score = scale * q.k;  softcap > 0: score = softcap * tanh(score / softcap);  slopes: score -= slopes[head] * |p - t|
- *   (softcap from 1e-6 |scale| to 1e30, with |scale| up to 1e12)
+ *   (softcap from 1e-30, and from 1e-6 |scale|, to 1e30, with |scale| up to 1e12)
  *   causal 1: t <= p.  window > 0 (causal only): also t > p - window.  causal 0: every position of the sequence.
  * (p = kv_len - new rows + index of the row; it may be negative: with causal 1 such a row sees nothing.) */
 typedef struct {

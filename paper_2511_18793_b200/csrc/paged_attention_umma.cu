@@ -642,10 +642,18 @@ bool launch_form(const PagedAttnArgs& a, int form, const CUtensorMap& tk, const 
 
 }  // namespace
 
-// false: not launched (no tensor map).
+// The series of a capped score goes in powers of the unscaled q.k, with coefficients down to scale (scale / softcap)^4: they have to be normal numbers, or terms
+// that count are lost (or are infinity times zero).  A cap of ordinary scores is far from that (scale 1/8: caps up to 1e8).
+static bool series_holds(const PagedAttnArgs& a) {
+  const double ratio = (double)a.scale / a.softcap, last = (double)kTanhShort[2] * a.scale * 1.4426950408889634 * ratio * ratio * ratio * ratio;
+  return fabs(last) >= 2e-38;
+}
+
+// false: not launched (no tensor map, or a cap that the series does not bear).
 bool launch_paged_attn_umma(const PagedAttnArgs& a, cudaStream_t st) {
   CUtensorMap tk{}, tv{};
   const int box = paged_box_rows(a.kv.page_size);
+  if (a.softcap > 0.f && !series_holds(a)) return false;
   if (box < 8 || !paged_map(a.kv, a.kv.k, box, &tk) || !paged_map(a.kv, a.kv.v, box, &tv)) return false;
   const int form = (a.softcap > 0.f ? kCap : 0) + (a.slopes || !(a.scale > 0.f) ? kBias : 0);
   const long long rows = (long long)a.kv.max_new * a.G;
