@@ -627,10 +627,12 @@ nezha_status device_error(nezha_ctx* c, const int* words) {
   if (st) NZ_CUDA(c, cudaMemsetAsync(c->es.status, 0, 4 * sizeof(int), c->st));
   if (st & kStHashFull) return fail(c, NEZHA_ERR_HASH_FULL, "hash set insertion exhausted its probe bound");
   if (st & kStBadCode) return fail(c, NEZHA_ERR_CATALOG, "a code outside [0, T_l) was given");
-  if (st & kStBadPage) return fail(c, NEZHA_ERR_PAGE, "paged cache: a page outside the pool, or a length, row range or position out of bounds");
-  if (st)      // a kernel that records where it gave up leaves three more words (0 if it does not)
+  const char* page = "paged cache: a page outside the pool, or a length, row range or position out of bounds";
+  if (st & ~kStBadPage)      // a kernel that records where it gave up leaves three more words (0 if it does not)
     return fail(c, NEZHA_ERR_CUDA, "a bounded device-side wait expired (kernel gave up and returned); where: " +
-                                       std::to_string(words[1]) + " " + std::to_string(words[2]) + " " + std::to_string(words[3]));
+                                       std::to_string(words[1]) + " " + std::to_string(words[2]) + " " + std::to_string(words[3]) +
+                                       (st & kStBadPage ? std::string("; and ") + page : ""));
+  if (st) return fail(c, NEZHA_ERR_PAGE, page);
   return NEZHA_OK;
 }
 nezha_status pending_device_error(nezha_ctx* c) {
