@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1) quantize_stream_kernel(cons
   __syncthreads();
   pdl_wait();
   pdl_launch();
-  const int first = blockIdx.x * G + group, step = gridDim.x * G, rows = first < M ? (M - first + step - 1) / step : 0;
+  const int first = blockIdx.x * G + group, step = gridDim.x * G, rows = first < M ? (M - 1 - first) / step + 1 : 0;
   auto bring = [&](int i) {
     const uint32_t bar = full_bar(i % stages);
     mbar_expect_tx(bar, row_bytes);
@@ -230,7 +230,7 @@ bool launch_stream(const T* x, long long x_stride, int M, int K, int8_t* q, floa
   if (stages < 2) return false;
   static PerDeviceOnce configured;
   configured.run([] { cudaFuncSetAttribute(quantize_stream_kernel<T, TPR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStreamBytes + kStreamHead<TPR> + 128); });
-  launch_pdl(quantize_stream_kernel<T, TPR>, dim3((unsigned)std::min(sm_count(), (M + kGroups<TPR> - 1) / kGroups<TPR>)), dim3(kStreamThreads),
+  launch_pdl(quantize_stream_kernel<T, TPR>, dim3((unsigned)std::min(sm_count(), (M - 1) / kGroups<TPR> + 1)), dim3(kStreamThreads),
              (size_t)stages * kGroups<TPR> * row_bytes + kStreamHead<TPR> + 128, st, x, x_stride, M, K, q, scale, stages, status);
   return true;
 }
@@ -251,7 +251,7 @@ void launch_t(const T* x, long long x_stride, int M, int K, int8_t* q, float* sc
   const auto go = [&](auto tpr, auto v) {
     constexpr int TPR = decltype(tpr)::value;
     constexpr int kRows = kBlock<TPR> / TPR;
-    launch_pdl(quantize_rows_kernel<T, TPR, decltype(v)::value>, dim3((M + kRows - 1) / kRows), dim3(kBlock<TPR>), 0, st, x, x_stride, M, K, q, scale);
+    launch_pdl(quantize_rows_kernel<T, TPR, decltype(v)::value>, dim3((M - 1) / kRows + 1), dim3(kBlock<TPR>), 0, st, x, x_stride, M, K, q, scale);
   };
   const auto pick = [&](auto v) {
     if (chunks <= 32 * 4) go(std::integral_constant<int, 32>{}, v);
