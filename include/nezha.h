@@ -373,8 +373,8 @@ nezha_status nezha_quantize_rows(nezha_ctx* ctx, const void* x, int64_t x_stride
 /* C[M, N] (op)= (sum_k A[m, k] W[n, k]) * a_scale[m] * w_scale[n] + bias[n]:  A int8 [M, K], W int8 [N, K], row-major and dense, -128 allowed.
  * The sum is exact (32-bit integer; K at most 131071), the rest in fp32.
  *   epilogue 0: C (storage type) = ;  1: C (float) = ;  2: C (float) +=           bias  device float [N] or NULL
- * The counterpart of nezha_gemm, which documents M, N, K.  Every size is served; the tensor cores want A and W 16-byte aligned and
- * K % 16 == 0.  The result does not depend on the kernel that serves it.  Asynchronous. */
+ * The counterpart of nezha_gemm, which documents M, N, K: at least 1; here M and N at most 2^31 - 256, and 2^31 tiles of 64 x 64 of C.  Every such size
+ * is served; the tensor cores want A and W 16-byte aligned and K % 16 == 0.  The result does not depend on the kernel that serves it.  Asynchronous. */
 nezha_status nezha_gemm_int8(nezha_ctx* ctx, const int8_t* A, const float* a_scale, const int8_t* W, const float* w_scale, void* C,
                              int32_t M, int32_t N, int32_t K, int32_t epilogue, const float* bias);
 

@@ -1365,7 +1365,9 @@ nezha_status nezha_gemm_int8(nezha_ctx* c, const int8_t* A, const float* a_scale
   if (!A || !a_scale || !W || !w_scale || !C || M < 1 || N < 1 || K < 1 || epilogue < 0 || epilogue > 2)
     return fail(c, NEZHA_ERR_ARG, "nezha_gemm_int8: bad argument");
   if (K > 131071) return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm_int8: sums of more than 131071 products do not fit 32 bits");
-  if ((int64_t)((M + 63) / 64) * ((N + 63) / 64) > INT32_MAX) return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm_int8: product too large for one call");
+  // (sizes are rounded up to whole tiles, of 256 at most, in 32 bits)
+  if (M > INT32_MAX - 255 || N > INT32_MAX - 255 || (int64_t)((M + 63) / 64) * ((N + 63) / 64) > INT32_MAX)
+    return fail(c, NEZHA_ERR_UNSUPPORTED, "nezha_gemm_int8: product too large for one call");
   if (((uintptr_t)C % (epilogue == 0 ? c->esz : 4)) || ((uintptr_t)a_scale & 3) || ((uintptr_t)w_scale & 3) || ((uintptr_t)bias & 3))
     return fail(c, NEZHA_ERR_ARG, "nezha_gemm_int8: a pointer is not aligned to its element");
   if (const nezha_status s = check_device(c, "nezha_gemm_int8")) return s;
