@@ -1249,7 +1249,8 @@ const char* attn_fault(const nezha_ctx* c, const nezha_paged_kv* kv, int32_t Hq,
   if (f->softcap > 0.f && (f->softcap < 1e-30f || f->softcap > 1e30f || std::fabs(f->scale) > 1e12f || std::fabs(f->scale) > 1e6f * f->softcap))
     return "softcap: at least 1e-30 and 1e-6 |scale|, at most 1e30, with a scale of at most 1e12";
   // a launch has a CTA per (KV head, row tile, split, sequence)
-  if ((double)kv->n_kv_heads * kv->batch * ((double)kv->max_new * (Hq / kv->n_kv_heads) / 16 + 1) > 2e8 || (int64_t)kv->rows * Hq > INT32_MAX)
+  if ((double)kv->n_kv_heads * kv->batch * ((double)kv->max_new * (Hq / kv->n_kv_heads) / 16 + 1) > 2e8 || (int64_t)kv->rows * Hq > INT32_MAX ||
+      (int64_t)kv->max_new * (Hq / kv->n_kv_heads) > INT32_MAX - 1023)      // (the end of the last tile of rows is counted in 32 bits)
     return "too many sequences, heads and rows for one call";
   return nullptr;
 }
