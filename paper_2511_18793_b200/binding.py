@@ -498,7 +498,7 @@ class Engine:
         st = t.stride()
         assert t.shape == (rows, heads, hd) and t.dtype is self._dtype and t.get_device() == self._dev
         assert st[2] == 1 and (st[1] == hd or heads == 1)
-        return st[0] if rows > 1 else max(st[0], heads * hd)
+        return st[0] if rows > 1 else heads * hd        # (of one row the stride says nothing)
 
     def rope_table(self, rope: Rope, n_positions: int) -> RopeTable:
         out = RopeTable(rope, self._new((n_positions, rope.rot_dim), torch.float32))
