@@ -255,8 +255,9 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_pair_kernel(const __grid_con
       drain<kPairN, OUT>(a, tmem_base + (uint32_t)(b * kPairN), q, half, lane, stg, m0, n0, wide, ts);
       tc_fence_before();
       __syncwarp();
-      // (relaxed: the accumulator has been read, and nothing in memory is handed over; a release would wait for the stores of C.  16,008 x 16,384 x 512:
-      // 240 us with one, 191 without; 8,634 x 2,336 x 832: 26.5, 22.5)
+      // (relaxed: nothing in memory is handed over, and a release would wait for the stores of C.  What the products behind it rest on is that the
+      // accumulator is in registers: tcgen05.wait::ld in the drain, and the fence before this.  16,008 x 16,384 x 512: 240 us with a release, 191
+      // without; 8,634 x 2,336 x 832: 26.5, 22.5)
       if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(acc_empty(b) & kLeaderMask) : "memory");
     }
     if (!ok && lane == 0) *abort_flag = 1;

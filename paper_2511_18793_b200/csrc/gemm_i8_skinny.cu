@@ -2,8 +2,9 @@
 // 128 rows of W are the MMA's 128-row operand and the rows of A its N (MT = 32, 64 or 128); an output tile is 128 columns of C.  The K range of a
 // tile is split over the CTAs of a cluster so that every SM streams a share of W.  Each CTA leaves its 32-bit sums in its own shared memory, where
 // the ring was; behind a cluster barrier the rows of the tile are dealt out to the warps of the cluster, which add the parts (whole
-// numbers: in any order the same) and store 128 neighbouring elements per row.  20 x 16,384 x 2,048: 11.3 us from HBM (W alone 5.3 at the copy's rate; the rest is the
-// start and the join), 5.8 from a warm L2.
+// numbers: in any order the same) and store 128 neighbouring elements per row.  20 x 16,384 x 2,048: 11.5 us from HBM (W alone 5.3 at the copy's rate),
+// 5.8 from a warm L2.  Its 128 tiles are a CTA each, so nothing is split or joined: 20 of the SMs have none, and the others have a ring of 100 KB, of which
+// 80 are W, because two CTAs per SM have to have room.
 #include "gemm_i8.cuh"
 
 namespace nz {

@@ -280,6 +280,7 @@ PagedAttnPlan paged_attn_plan(const PagedAttnArgs& a, bool bf16) {
     int tile_rows = kRowsS, per_sm = 4, least = 2;
     if (bf16 && a.kv.hd >= 64) {
       p.kernel = rows <= 8 ? kToken : rows <= 16 ? kTc16 : kTc64;
+      // (three waves of the three CTAs that an SM holds; of 9 to 16 rows with heads of 128 it holds two, which makes it four and a half)
       tile_rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 64;
       per_sm = rows <= 16 ? 9 : 2;
       least = rows <= 16 ? 8 : 4;

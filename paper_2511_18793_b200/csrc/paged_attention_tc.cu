@@ -1,14 +1,16 @@
 // Attention over a paged cache on mma.sync (bf16, heads of 64 and 128): calls of few query rows, which are bound by reading keys and values
-// once, and page sizes that the tcgen05 kernel does not take.
+// once, and what the tcgen05 kernel does not take (page sizes that are no multiple of 8, caps that its series does not bear).
 //
 // A CTA has one (sequence, KV head), a tile of 16 RW query rows (tokens times the heads of the group) and a share of the context.  A producer
 // warp brings tiles of 64 positions into a ring: by TMA, one box of 64 columns per page or piece of a page, where the page size is a
 // multiple of 8, else 16 bytes at a time (cp.async), positions that no row sees as zeros.  RW row warps x KW position groups compute
 // S = Q K^T and O += P V in registers with a running maximum and sum; the KW groups take every KW-th tile and are merged at the end.
-// One token per sequence: RW = 1, KW = 2, 64 KB of ring, three CTAs per SM -- a warp's chain (scores, softmax, second product) takes about
-// as long as a tile's way from HBM, so six of them per SM keep the memory busy.
-// 64 tokens of 32 heads of 128 on 8, on up to 4,000 positions in pages of 16: 126 us, 5.5 TB/s of the copy's 6.5 (113 with a warm L2); one token on 32k
-// positions, heads of 64: 24 us with the join, of which the stream is 10.
+// 9 to 16 rows: RW = 1, KW = 2, 64 KB of ring; three CTAs per SM with heads of 64, two with heads of 128, whose 208 registers a thread (plain; 247 capped or
+// biased) leave room for eight warps.  One token of 16 heads of 128 on one, 64 sequences on up to 4,000 positions: 31 us, floor 13 (the bytes).
+// 17 to 64 rows: RW = 4, KW = 1.  Ten tokens of 32 heads on 8, 32 sequences on up to 4,000 positions: heads of 128 130 us, floor 55; heads of 64 64, 28.
+// At most 8 rows (the last kernel here): three CTAs per SM -- a warp's chain (scores, softmax, second product) takes about as long as a tile's way from HBM,
+// so six or more of them per SM keep the memory busy.  64 tokens of 32 heads of 128 on 8, on up to 4,000 positions in pages of 16: 126 us, 5.5 TB/s of the
+// copy's 6.5 (113 with a warm L2; pages of 20, by 16-byte copies: 212); one token on 32k positions, heads of 64: 24 us with the join, of which the stream is 10.
 //
 // What a row does not see has no part in its sums: scores are replaced, not added to; values at positions outside what the CTA's rows see
 // are zeroed in the tile, and where only some of its rows see a position, values that are not finite are taken out of the tile and added to
