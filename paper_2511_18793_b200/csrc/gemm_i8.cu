@@ -199,13 +199,13 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_pair_kernel(const __grid_con
 
   if (warp == 0) {
     const uint32_t leader = elect_one();
-    int s = 0;
+    int it = 0, s = 0;
     uint32_t round = 0;
     bool ok = true;
     for (int tile = pair; tile < n_tiles && ok; tile += n_pairs) {
       const TileMN tt = tile_of(tile, tiles_m, tiles_n, band);
       const int m0 = tt.m * 256 + (int)rank * 128, nb0 = tt.n * kPairN + (int)rank * 128;
-      for (int k = 0; k < k_iters; ++k) {
+      for (int k = 0; k < k_iters; ++k, ++it) {
         if (!warp_wait_uniform(empty_bar(s), round ^ 1u, abort_flag)) { ok = false; break; }
         const uint32_t dst = base + s * kPairStage, fb = full_bar(s) & kLeaderMask;
         mbar_expect_tx_if(full_bar(s), 2 * kPairStage, rank == 0 ? leader : 0u);
@@ -214,7 +214,12 @@ __global__ void __launch_bounds__(kThreads) gemm_i8_pair_kernel(const __grid_con
         if (++s == STAGES) { s = 0; round ^= 1u; }
       }
     }
-    if (!ok && lane == 0) *abort_flag = 1;
+    // (both CTAs' copies arrive on the leader's barriers: it waits for those in flight, and the other for it, at the cluster's barrier)
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (rank == 0)
+        for (int j = max(0, it - STAGES); j < it; ++j) mbar_wait(full_bar(j % STAGES), (j / STAGES) & 1);
+    }
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t leader = elect_one();
